@@ -1,0 +1,598 @@
+// lsm_prefix_attention: attention over a paged cache for batches whose requests share long prefixes.
+//
+// A row is one query head of one new token.  Rows of a KV head that see the same keys are packed into tiles, whatever request they
+// belong to: behind a shared prefix these are the rows of the whole group, behind a request's own pages those of the request.
+// A workgroup takes a tile of rows and a range of keys and goes over the keys once with a running maximum and sum; where a tile's
+// keys are dealt to several workgroups (the prefix and the own pages always are, unless rows are packed by request anyway), each
+// leaves its accumulator, maximum and sum, and a second kernel joins them in a fixed order.
+#include <hip/hip_runtime.h>
+
+#include "lsm_cache.h"
+#include "lsm_common.h"
+
+namespace lsm {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int kType>
+struct Half;
+template <>
+struct Half<LSM_BF16> {
+    typedef __bf16 type;
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Half<LSM_FP16> {
+    typedef _Float16 type;
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+constexpr uint32_t kThreads = 256, kWaves = kThreads / kWave;
+constexpr uint32_t kWaveRows = 32;                      // rows of a wave: the columns of one product
+constexpr uint32_t kWideRows = kWaveRows * kWaves;      // a wide tile: each wave has rows of its own, all go over the same keys
+constexpr uint32_t kNarrowRows = kWaveRows;             // a narrow tile: all waves have the same rows, each goes over keys of its own
+constexpr uint32_t kSplitKeys = 64;                     // ranges of keys are whole numbers of this
+
+struct AttentionArgs {
+    const void* q;
+    void* out;
+    float* lse;
+    const void *k, *v;
+    int64_t q_token, q_head, out_token, out_head, k_page, k_token, k_head, v_page, v_token, v_head;
+    const int32_t *group_offsets, *prefix_tables, *prefix_lens, *q_offsets, *own_tables, *own_lens;
+    uint32_t n_tokens, n_requests, n_groups, n_pages, page_shift, kv_heads, share, rows;
+    uint64_t prefix_width, own_width;
+    float scale;  // of the exponent of two
+    // The plan.  Stage 0: rows packed by group over the prefix; stage 1: rows packed by request over its own pages, or over the
+    // prefix and its own pages (`whole`).
+    uint32_t whole, tiles[2], splits[2], wide[2];
+    uint32_t joined;  // the parts are joined by another kernel
+    float* part_out;  // [split of either stage][row][head_dim]
+    float2* part_ml;  // [split of either stage][row]: maximum in units of the exponent of two, sum
+};
+
+// Keys in [0, length), in ranges of at least two splitting units; how many there are.
+__device__ __forceinline__ uint32_t split_units(uint32_t units, uint32_t splits) {
+    const uint32_t each = (units + splits - 1) / splits;
+    return each < 2 ? 2 : each;
+}
+__device__ __forceinline__ uint32_t real_splits(uint32_t units, uint32_t splits) {
+    const uint32_t each = split_units(units, splits);
+    return (units + each - 1) / each;
+}
+__device__ __forceinline__ uint32_t units_of(uint32_t keys) { return (keys + kSplitKeys - 1) / kSplitKeys; }
+
+__device__ __forceinline__ uint32_t clamp_u32(int32_t v, uint64_t most) { return v < 0 ? 0 : (uint64_t)v > most ? (uint32_t)most : (uint32_t)v; }
+__device__ __forceinline__ uint32_t prefix_len(const AttentionArgs& a, uint32_t g) { return clamp_u32(a.prefix_lens[g], a.prefix_width << a.page_shift); }
+__device__ __forceinline__ uint32_t own_len(const AttentionArgs& a, uint32_t r) { return clamp_u32(a.own_lens[r], a.own_width << a.page_shift); }
+__device__ __forceinline__ uint32_t token_of_request(const AttentionArgs& a, uint32_t r) { return clamp_u32(a.q_offsets[r], a.n_tokens); }
+__device__ __forceinline__ uint32_t token_of_group(const AttentionArgs& a, uint32_t g) { return token_of_request(a, clamp_u32(a.group_offsets[g], a.n_requests)); }
+
+// The last i < n with start(i) <= x, for start(0) <= x and start not descending; every lane of the wave calls and gets it.
+template <typename F>
+__device__ __forceinline__ uint32_t last_not_above(uint32_t n, uint64_t x, F start) {
+    const uint32_t lane = threadIdx.x & (kWave - 1);
+    uint32_t count = 0;
+    for (uint32_t base = 0; base < n; base += kWave) {
+        const uint32_t i = base + lane;
+        const uint64_t ok = __ballot(i < n && start(i) <= x);
+        count += (uint32_t)__popcll(ok);
+        if (ok != ~0ull) break;
+    }
+    return count > 0 ? count - 1 : 0;
+}
+__device__ __forceinline__ uint32_t group_of(const AttentionArgs& a, uint32_t request) {
+    return last_not_above(a.n_groups, request, [&](uint32_t g) { return (uint64_t)clamp_u32(a.group_offsets[g], a.n_requests); });
+}
+
+// exchange with the lane 32 further or back
+__device__ __forceinline__ float other_half_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float other_half_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// What a workgroup works on.
+struct Item {
+    uint32_t row0, row_end;        // rows [row0, row_end) of the KV head
+    const int32_t* table[2];       // pages of the two segments of keys: the prefix, the request's own
+    uint32_t len[2];               // their lengths
+    uint32_t unit0, unit1;         // splitting units of this range; the first segment has units_of(len[0]) of them
+    uint32_t part;                 // which part it leaves
+    uint32_t token0, hidden;       // own keys that token t sees: t - token0 + 1 + len[1] - (new tokens), as hidden = that for t = token0, minus 1, wrapped
+};
+
+// A team of kTeam waves goes over tiles of kKeys keys: copies them through LDS and multiplies.  kHead = head_dim.
+//
+// Scores are computed transposed, keys times queries, so that a lane holds scores of one row (row = lane % 32) and the
+// running maximum and sum are a lane's own, but for one exchange with the lane 32 away.  The lane's scores, rounded, are in the
+// layout that the second product, values transposed times weights, wants as its right operand if its sum over keys takes them in the order
+// 0-3, 8-11 | 4-7, 12-15 of every 16; its left operand, four keys at a time of one column of the values, is what the transposing LDS read gives.
+// In LDS the 16-byte words of a row are permuted by the row's number so that neither read has bank conflicts.
+template <int kType, int kHead, int kTeam, int kKeys>
+struct Team {
+    typedef typename Half<kType>::type T;
+    typedef typename Half<kType>::x8 x8;
+    static constexpr uint32_t kWords = kHead / 8;                                 // 16-byte words of a row
+    static constexpr uint32_t kLoads = kKeys * kWords / (kTeam * kWave);          // words a lane copies of the keys of a tile, and of the values
+    static constexpr uint32_t kRowsPerLoad = kTeam * kWave / kWords;
+    static constexpr uint32_t kBytes = kKeys * kHead * 2;                         // of a tile of keys, or of values
+    static_assert(kKeys * kWords % (kTeam * kWave) == 0 && kKeys % 32 == 0 && kKeys <= 64, "");
+
+    static __device__ __forceinline__ uint32_t key_word(uint32_t row, uint32_t word) {  // where a 16-byte word of a key's row is
+        return kWords >= 16 ? word ^ (row & 15) : word ^ ((row >> 1) & 7);
+    }
+    static __device__ __forceinline__ uint32_t value_word(uint32_t row, uint32_t word) {
+        const uint32_t by = kWords >= 16 ? 2 * (row & 3) + ((row >> 2) & 1) : 2 * ((row >> 1) & 1) + ((row >> 2) & 1);
+        return word ^ (by * 2);
+    }
+
+    x8 query[kHead / 16];
+    f32x16 acc[kHead / 32];
+    float most, sum;  // maximum of the row so far in units of the exponent of two; this lane's share of the sum
+
+    __device__ __forceinline__ void start() {
+#pragma unroll
+        for (uint32_t i = 0; i < kHead / 32; i++)
+#pragma unroll
+            for (int j = 0; j < 16; j++) acc[i][j] = 0.f;
+        most = -__builtin_inff(), sum = 0.f;
+    }
+
+    // One tile: keys and values are in LDS.  present: which of its keys there are; limit: how many of them this lane's row may see.
+    __device__ __forceinline__ void tile(const char* keys, const char* values, uint64_t present, int32_t limit, bool masked, float scale) {
+        const uint32_t lane = threadIdx.x & (kWave - 1), n = lane & 31, h = lane >> 5;
+        f32x16 s[kKeys / 32];
+#pragma unroll
+        for (int b = 0; b < kKeys / 32; b++) {
+#pragma unroll
+            for (int j = 0; j < 16; j++) s[b][j] = 0.f;
+            const uint32_t row = b * 32 + n;
+#pragma unroll
+            for (uint32_t c = 0; c < kHead / 16; c++) {
+                const x8 k = *reinterpret_cast<const x8*>(keys + row * kHead * 2 + key_word(row, 2 * c + h) * 16);
+                s[b] = Half<kType>::mfma(k, query[c], s[b]);
+            }
+        }
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < kKeys / 32; b++) {
+                const int32_t rest = limit - b * 32;
+                uint32_t see = rest <= 0 ? 0 : rest >= 32 ? ~0u : (1u << rest) - 1;
+                see = (see & (uint32_t)(present >> (b * 32))) >> (4 * h);
+#pragma unroll
+                for (int j = 0; j < 16; j++) s[b][j] = (see >> (8 * (j / 4) + j % 4)) & 1 ? s[b][j] : -__builtin_inff();
+            }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < kKeys / 32; b++)
+#pragma unroll
+            for (int j = 0; j < 16; j++) top = fmaxf(top, s[b][j]);
+        top = other_half_max(top) * scale;
+        const float now = fmaxf(most, top);
+        if (__any(now > most)) {
+            const float by = now > most ? __builtin_amdgcn_exp2f(most - now) : 1.f;
+            sum *= by;
+#pragma unroll
+            for (uint32_t i = 0; i < kHead / 32; i++)
+#pragma unroll
+                for (int j = 0; j < 16; j++) acc[i][j] *= by;
+            most = now;
+        }
+        const float base = most == -__builtin_inff() ? 0.f : most;  // a row that has seen nothing: all weights 0
+        x8 p[kKeys / 16];
+#pragma unroll
+        for (int b = 0; b < kKeys / 32; b++)
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, -base));
+                sum += e;
+                p[b * 2 + j / 8][j % 8] = (T)e;
+            }
+        // values: 16 lanes read a block of 4 keys x 16 columns, lane i of them gets column i
+        const uint32_t i16 = lane & 15, column = ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
+#pragma unroll
+        for (uint32_t d = 0; d < kHead / 32; d++) {
+#pragma unroll
+            for (uint32_t b = 0; b < kKeys / 16; b++) {
+                union {
+                    x8 all;
+                    s16x4 part[2];
+                } u;
+#pragma unroll
+                for (uint32_t j = 0; j < 2; j++) {
+                    const uint32_t row = b * 16 + 8 * j + 4 * h + (i16 >> 2), at = d * 32 + column;
+                    const char* from = values + row * kHead * 2 + value_word(row, at >> 3) * 16 + (at & 4) * 2;
+                    u.part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from));
+                }
+                acc[d] = Half<kType>::mfma(u.all, p[b], acc[d]);
+            }
+        }
+    }
+};
+
+// kType, kHead as above.  A wide tile's keys are copied by all waves together, a narrow one's by each wave for itself.
+template <int kType, int kHead>
+struct Shape {
+    static constexpr int kWideKeys = kHead == 256 ? 32 : 64, kNarrowKeys = kHead == 64 ? 64 : 32;
+    typedef Team<kType, kHead, kWaves, kWideKeys> Wide;
+    typedef Team<kType, kHead, 1, kNarrowKeys> Narrow;
+    static constexpr uint32_t kLds = Wide::kBytes * 2 > Narrow::kBytes * 2 * kWaves ? Wide::kBytes * 2 : Narrow::kBytes * 2 * kWaves;
+    static constexpr uint32_t kSlicePitch = 68;  // floats between rows of a slice of 64 columns of results in LDS
+    static_assert(kWaves * 32 * kSlicePitch * 4 + kWaves * 32 * 8 <= 160 * 1024, "");
+    static constexpr uint32_t kOutLds = kWaves * 32 * kSlicePitch * 4 + kWaves * 32 * 8;
+    static constexpr uint32_t kAllLds = kLds > kOutLds ? kLds : kOutLds;
+};
+
+template <int kType, int kHead, bool kWide>
+__device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, uint32_t kv_head, char* lds) {
+    typedef Shape<kType, kHead> S;
+    typedef typename Half<kType>::type T;
+    typedef typename Half<kType>::x8 x8;
+    constexpr int kTeam = kWide ? kWaves : 1, kKeys = kWide ? S::kWideKeys : S::kNarrowKeys;
+    typedef Team<kType, kHead, kTeam, kKeys> X;
+    constexpr uint32_t kPerUnit = kSplitKeys / kKeys;
+    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1), n = lane & 31, h = lane >> 5;
+    const uint32_t in_team = kWide ? threadIdx.x : lane;
+    char* keys = lds + (kWide ? 0 : wave * 2 * X::kBytes);
+    char* values = keys + X::kBytes;
+
+    X x;
+    x.start();
+    const uint32_t row = w.row0 + (kWide ? wave * 32 : 0) + n;
+    const bool has_row = row < w.row_end;
+    const uint32_t token = row / a.share, head = kv_head * a.share + (row - token * a.share);
+    {
+        const T* from = static_cast<const T*>(a.q) + (int64_t)token * a.q_token + (int64_t)head * a.q_head + h * 8;
+#pragma unroll
+        for (uint32_t c = 0; c < kHead / 16; c++) {
+            if (has_row) {
+                x.query[c] = *reinterpret_cast<const x8*>(from + c * 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; j++) x.query[c][j] = (T)0.f;
+            }
+        }
+    }
+    const int32_t sees = (int32_t)(token - w.token0 + w.hidden) + 1;  // own keys this row sees
+    // tiles of this range: of the first segment, then of the second as far as any row of the tile sees
+    const uint32_t units0 = units_of(w.len[0]), last_row = w.row_end < w.row0 + (kWide ? kWideRows : kNarrowRows) ? w.row_end - 1 : w.row0 + (kWide ? kWideRows : kNarrowRows) - 1;
+    const uint32_t first_row = w.row0 + (kWide ? wave * 32 : 0);
+    const int32_t most_seen = (int32_t)(last_row / a.share - w.token0 + w.hidden) + 1;
+    const int32_t least_seen = (int32_t)(first_row / a.share - w.token0 + w.hidden) + 1;  // of the rows of this wave
+    const uint32_t seen = most_seen < 0 ? 0 : (uint32_t)most_seen < w.len[1] ? (uint32_t)most_seen : w.len[1];
+    const uint32_t units = units0 + units_of(seen);
+    const uint32_t unit1 = w.unit1 < units ? w.unit1 : units;
+    const uint32_t tile_end = unit1 * kPerUnit, step = kWide ? 1 : kWaves;
+    uint32_t t = w.unit0 * kPerUnit + (kWide ? 0 : wave);
+
+    const T* k_head = static_cast<const T*>(a.k) + (int64_t)kv_head * a.k_head;
+    const T* v_head = static_cast<const T*>(a.v) + (int64_t)kv_head * a.v_head;
+    const uint32_t page_mask = (1u << a.page_shift) - 1;
+
+    // the page of key `lane` of tile t, or -1
+    auto page_of = [&](uint32_t t) -> int32_t {
+        const uint32_t seg = t >= units0 * kPerUnit ? 1 : 0;
+        const uint32_t at = (t - (seg ? units0 * kPerUnit : 0)) * kKeys + lane;
+        const uint32_t len = seg ? seen : w.len[0];
+        if (t >= tile_end || lane >= (uint32_t)kKeys || at >= len) return -1;
+        const int32_t page = w.table[seg][at >> a.page_shift];
+        return (uint32_t)page < a.n_pages ? page : -1;
+    };
+    uint4 kr[X::kLoads], vr[X::kLoads];
+    auto load = [&](uint32_t t, int32_t page) {  // page: of key `lane`
+        const uint32_t seg = t >= units0 * kPerUnit ? 1 : 0;
+        const uint32_t at = (t - (seg ? units0 * kPerUnit : 0)) * kKeys;
+#pragma unroll
+        for (uint32_t i = 0; i < X::kLoads; i++) {
+            const uint32_t r = i * X::kRowsPerLoad + in_team / X::kWords, c = in_team % X::kWords;
+            const int32_t p = __shfl(page, (int)r, kWave);
+            const int64_t slot = (at + r) & page_mask;
+            kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+            if (p >= 0) {
+                kr[i] = load_global_u4(reinterpret_cast<const uint4*>(k_head + p * a.k_page + slot * a.k_token + c * 8));
+                vr[i] = load_global_u4(reinterpret_cast<const uint4*>(v_head + p * a.v_page + slot * a.v_token + c * 8));
+            }
+        }
+    };
+    int32_t page = page_of(t), next_page = page_of(t + step);
+    if (t < tile_end) load(t, page);
+    for (; t < tile_end; t += step) {
+#pragma unroll
+        for (uint32_t i = 0; i < X::kLoads; i++) {
+            const uint32_t r = i * X::kRowsPerLoad + in_team / X::kWords, c = in_team % X::kWords;
+            *reinterpret_cast<uint4*>(keys + r * kHead * 2 + X::key_word(r, c) * 16) = kr[i];
+            *reinterpret_cast<uint4*>(values + r * kHead * 2 + X::value_word(r, c) * 16) = vr[i];
+        }
+        if (kWide) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
+        const uint64_t present = __ballot(page >= 0);
+        page = next_page;
+        if (t + step < tile_end) load(t + step, page);
+        next_page = page_of(t + 2 * step);
+        const bool second = t >= units0 * kPerUnit;
+        const int32_t limit = second ? sees - (int32_t)((t - units0 * kPerUnit) * kKeys) : kKeys;
+        const bool masked = present != (kKeys == 64 ? ~0ull : (1ull << kKeys) - 1) || (second && least_seen < (int32_t)((t - units0 * kPerUnit + 1) * kKeys));
+        x.tile(keys, values, present, limit, masked, a.scale);
+        if (kWide) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
+    }
+    x.sum = other_half_sum(x.sum);
+
+    // Results go through LDS, 64 columns at a time, to be written in whole rows; a narrow tile's waves are joined on the way.
+    float* slices = reinterpret_cast<float*>(lds);
+    float2* ml = reinterpret_cast<float2*>(lds + kWaves * 32 * S::kSlicePitch * 4);
+    float by = 1.f, most = x.most, sum = x.sum;
+    __syncthreads();
+    if (!kWide) {
+        if (h == 0) ml[wave * 32 + n] = make_float2(x.most, x.sum);
+        __syncthreads();
+        float2 each[kWaves];
+        most = -__builtin_inff();
+#pragma unroll
+        for (uint32_t i = 0; i < kWaves; i++) each[i] = ml[i * 32 + n], most = fmaxf(most, each[i].x);
+        const float base = most == -__builtin_inff() ? 0.f : most;
+        sum = 0.f;
+#pragma unroll
+        for (uint32_t i = 0; i < kWaves; i++) sum += each[i].y * __builtin_amdgcn_exp2f(each[i].x - base);
+        by = __builtin_amdgcn_exp2f(x.most - base);
+    }
+    if (!a.joined) by *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    const uint64_t place = (uint64_t)w.part * a.rows * a.kv_heads;  // rows of all KV heads: token by token, all heads of a token
+    if (has_row && h == 0 && (kWide || wave == 0)) {
+        const uint64_t at = (uint64_t)token * a.share * a.kv_heads + head;
+        if (a.joined) a.part_ml[place + at] = make_float2(most, sum);
+        else if (a.lse != nullptr) a.lse[at] = sum == 0.f ? -__builtin_inff() : (most + log2f(sum)) * 0.69314718055994531f;
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < kHead / 64; s++) {
+#pragma unroll
+        for (uint32_t d = 0; d < 2; d++)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                const f32x16& v = x.acc[s * 2 + d];
+                float4 o = make_float4(v[j * 4] * by, v[j * 4 + 1] * by, v[j * 4 + 2] * by, v[j * 4 + 3] * by);
+                *reinterpret_cast<float4*>(slices + (wave * 32 + n) * S::kSlicePitch + d * 32 + j * 8 + h * 4) = o;
+            }
+        __syncthreads();
+        // eight columns a thread
+        for (uint32_t u = threadIdx.x; u < (kWide ? kWideRows : kNarrowRows) * 8; u += kThreads) {
+            const uint32_t r = u >> 3, c = (u & 7) * 8;
+            if (w.row0 + r >= w.row_end) break;
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) o[j] = slices[r * S::kSlicePitch + c + j];
+            if (!kWide) {
+#pragma unroll
+                for (uint32_t i = 1; i < kWaves; i++)
+#pragma unroll
+                    for (int j = 0; j < 8; j++) o[j] += slices[(i * 32 + r) * S::kSlicePitch + c + j];
+            }
+            const uint32_t tok = (w.row0 + r) / a.share, hd = kv_head * a.share + (w.row0 + r - tok * a.share);
+            if (a.joined) {
+                float* to = a.part_out + (place + (uint64_t)tok * a.share * a.kv_heads + hd) * kHead + s * 64 + c;
+                *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            } else {
+                x8 v;
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[j] = (T)o[j];
+                *reinterpret_cast<x8*>(static_cast<T*>(a.out) + (int64_t)tok * a.out_token + (int64_t)hd * a.out_head + s * 64 + c) = v;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int kType, int kHead>
+__global__ void __launch_bounds__(kThreads, kHead == 256 ? 1 : 2) attention_kernel(const AttentionArgs a) {
+    __shared__ __attribute__((aligned(16))) char lds[Shape<kType, kHead>::kAllLds];
+    uint32_t b = blockIdx.x;
+    const uint32_t items0 = a.tiles[0] * a.splits[0] * a.kv_heads, stage = b >= items0 ? 1 : 0;
+    if (stage) b -= items0;
+    const uint32_t kv_head = b % a.kv_heads, tile = b / a.kv_heads % a.tiles[stage], split = b / a.kv_heads / a.tiles[stage];
+    const bool wide = a.wide[stage] != 0;
+    const uint32_t tile_rows = wide ? kWideRows : kNarrowRows;
+    // Owner i of rows [offset(i), offset(i + 1)) has the tiles from offset(i) / tile_rows + i on: at least as many as it needs, at no one else's place
+    Item w;
+    uint32_t owner, begin, end;
+    if (stage == 0) {
+        owner = last_not_above(a.n_groups, tile, [&](uint32_t g) { return (uint64_t)token_of_group(a, g) * a.share / tile_rows + g; });
+        begin = token_of_group(a, owner), end = token_of_group(a, owner + 1);
+    } else {
+        owner = last_not_above(a.n_requests, tile, [&](uint32_t r) { return (uint64_t)token_of_request(a, r) * a.share / tile_rows + r; });
+        begin = token_of_request(a, owner), end = token_of_request(a, owner + 1);
+    }
+    const uint64_t row0 = (uint64_t)begin * a.share + (uint64_t)(tile - ((uint64_t)begin * a.share / tile_rows + owner)) * tile_rows;
+    if (end <= begin || row0 >= (uint64_t)end * a.share) return;
+    w.row0 = (uint32_t)row0;
+    w.row_end = end * a.share;
+    if (stage == 0) {
+        w.table[0] = a.prefix_tables + owner * a.prefix_width, w.len[0] = prefix_len(a, owner);
+        w.table[1] = nullptr, w.len[1] = 0;
+    } else {
+        w.len[0] = 0, w.table[0] = nullptr;
+        if (a.whole && a.prefix_width != 0) {
+            const uint32_t g = group_of(a, owner);
+            w.table[0] = a.prefix_tables + g * a.prefix_width, w.len[0] = prefix_len(a, g);
+        }
+        w.table[1] = a.own_tables + owner * a.own_width, w.len[1] = own_len(a, owner);
+    }
+    w.token0 = begin;
+    w.hidden = w.len[1] - (end - begin);
+    const uint32_t units = units_of(w.len[0]) + units_of(w.len[1]), each = split_units(units, a.splits[stage]);
+    w.unit0 = split * each, w.unit1 = w.unit0 + each < units ? w.unit0 + each : units;
+    if (a.joined && w.unit0 >= units) return;  // not one of the ranges that there are
+    w.part = (stage ? a.splits[0] : 0) + split;
+    if (wide) attend<kType, kHead, true>(a, w, kv_head, lds);
+    else attend<kType, kHead, false>(a, w, kv_head, lds);
+}
+
+// Joins a row's parts: those of its prefix, then those of its own pages, each in the order of the keys.  kHead / 4 lanes have a row.
+template <int kType, int kHead>
+__global__ void __launch_bounds__(kThreads) join_kernel(const AttentionArgs a) {
+    typedef typename Half<kType>::type T;
+    constexpr uint32_t kLanes = kHead / 4, kRows = kWave / kLanes;  // rows of a wave
+    const uint32_t lane = threadIdx.x & (kWave - 1), heads = a.share * a.kv_heads;
+    const uint64_t all = (uint64_t)a.n_tokens * heads;
+    const uint64_t first = ((uint64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kRows;
+    if (first >= all) return;
+    uint64_t at = first + lane / kLanes;
+    const bool mine = at < all;
+    if (!mine) at = all - 1;
+    const uint32_t token = (uint32_t)(at / heads), head = (uint32_t)(at - (uint64_t)token * heads), c = (lane % kLanes) * 4;
+    // a wave's rows may belong to two tokens, and these to two requests
+    const uint32_t token_a = (uint32_t)(first / heads);
+    uint32_t request = last_not_above(a.n_requests, token_a, [&](uint32_t r) { return (uint64_t)token_of_request(a, r); });
+    while (request + 1 < a.n_requests && token_of_request(a, request + 1) <= token) request++;
+    uint32_t parts[2], from[2] = {0, a.splits[0]};
+    uint32_t g = 0;
+    if (a.prefix_width != 0) {
+        const uint32_t first_request = (uint32_t)__builtin_amdgcn_readfirstlane((int)request);
+        g = group_of(a, first_request);
+        while (g + 1 < a.n_groups && clamp_u32(a.group_offsets[g + 1], a.n_requests) <= request) g++;
+    }
+    const uint32_t units0 = a.prefix_width != 0 ? units_of(prefix_len(a, g)) : 0, units1 = units_of(own_len(a, request));
+    parts[0] = a.whole ? 0 : real_splits(units0, a.splits[0]);
+    parts[1] = real_splits(units1 + (a.whole ? units0 : 0), a.splits[1]);
+    float most = -__builtin_inff(), sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t stage = 0; stage < 2; stage++)
+        for (uint32_t i = 0; i < parts[stage]; i++) {
+            const uint64_t place = (uint64_t)(from[stage] + i) * all + at;
+            const float2 ml = a.part_ml[place];
+            const float4 v = *reinterpret_cast<const float4*>(a.part_out + place * kHead + c);
+            const float now = fmaxf(most, ml.x), base = now == -__builtin_inff() ? 0.f : now;
+            const float old_by = __builtin_amdgcn_exp2f(most - base), new_by = __builtin_amdgcn_exp2f(ml.x - base);
+            sum = sum * old_by + ml.y * new_by;
+            o.x = o.x * old_by + v.x * new_by, o.y = o.y * old_by + v.y * new_by;
+            o.z = o.z * old_by + v.z * new_by, o.w = o.w * old_by + v.w * new_by;
+            most = now;
+        }
+    if (!mine) return;
+    const float by = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    typedef T x4 __attribute__((ext_vector_type(4)));
+    x4 r;
+    r[0] = (T)(o.x * by), r[1] = (T)(o.y * by), r[2] = (T)(o.z * by), r[3] = (T)(o.w * by);
+    *reinterpret_cast<x4*>(static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + c) = r;
+    if (a.lse != nullptr && lane % kLanes == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (most + log2f(sum)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------------------------------
+static bool aligned_rows(const void* data, int64_t s0, int64_t s1, int64_t s2) {
+    return ((reinterpret_cast<uint64_t>(data) | (uint64_t)(s0 * 2) | (uint64_t)(s1 * 2) | (uint64_t)(s2 * 2)) & 15) == 0;
+}
+
+static int check_attention(const lsm_attention_t* a) {
+    if (a == nullptr) return LSM_ERR_NULL;
+    if (a->dtype != LSM_BF16 && a->dtype != LSM_FP16) return LSM_ERR_BAD_ARG;
+    if (a->head_dim != 64 && a->head_dim != 128 && a->head_dim != 256) return LSM_ERR_BAD_ARG;
+    if (a->page_tokens < LSM_MIN_PAGE_TOKENS || a->page_tokens > LSM_MAX_PAGE_TOKENS || (a->page_tokens & (a->page_tokens - 1)) != 0) return LSM_ERR_BAD_ARG;
+    if (a->kv_heads == 0 || a->q.heads == 0 || a->q.heads != a->out.heads || a->q.heads % a->kv_heads != 0 || a->q.heads > 4096) return LSM_ERR_BAD_ARG;
+    if (a->n_tokens >= 1u << 24 || a->n_tokens * a->q.heads >= 1ull << 31 || a->n_requests >= 1u << 24 || a->n_groups >= 1u << 24 || a->n_pages >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (a->prefix_width * a->page_tokens >= 1ull << 30 || a->own_width * a->page_tokens >= 1ull << 30 || a->prefix_width >= 1u << 30 || a->own_width >= 1u << 30) return LSM_ERR_BAD_ARG;
+    if (a->reserved != 0 || !(a->scale > 0.f) || a->scale > 3.0e38f) return LSM_ERR_BAD_ARG;
+    if (a->n_tokens == 0) return LSM_OK;
+    if (a->n_requests == 0) return LSM_ERR_BAD_ARG;
+    if (a->q.data == nullptr || a->out.data == nullptr || a->q_offsets == nullptr || a->own_lens == nullptr) return LSM_ERR_NULL;
+    if (a->own_width != 0 && a->own_tables == nullptr) return LSM_ERR_NULL;
+    if (a->prefix_width != 0 && a->n_groups != 0 && (a->prefix_tables == nullptr || a->prefix_lens == nullptr || a->group_offsets == nullptr)) return LSM_ERR_NULL;
+    if (a->n_pages != 0 && (a->k_pages.data == nullptr || a->v_pages.data == nullptr)) return LSM_ERR_NULL;
+    if (!aligned_rows(a->q.data, a->q.token_stride, a->q.head_stride, 0) || !aligned_rows(a->out.data, a->out.token_stride, a->out.head_stride, 0) ||
+        !aligned_rows(a->k_pages.data, a->k_pages.page_stride, a->k_pages.token_stride, a->k_pages.head_stride) ||
+        !aligned_rows(a->v_pages.data, a->v_pages.page_stride, a->v_pages.token_stride, a->v_pages.head_stride)) return LSM_ERR_BAD_ARG;
+    const uint64_t words = reinterpret_cast<uint64_t>(a->lse) | reinterpret_cast<uint64_t>(a->group_offsets) | reinterpret_cast<uint64_t>(a->prefix_tables) |
+                           reinterpret_cast<uint64_t>(a->prefix_lens) | reinterpret_cast<uint64_t>(a->q_offsets) | reinterpret_cast<uint64_t>(a->own_tables) |
+                           reinterpret_cast<uint64_t>(a->own_lens);
+    return words & 3 ? LSM_ERR_BAD_ARG : LSM_OK;
+}
+
+// How the work is cut; from sizes that the host knows.
+static void plan_attention(const lsm_attention_t* a, AttentionArgs& p) {
+    const uint64_t share = a->q.heads / a->kv_heads, rows = a->n_tokens * share;
+    const uint64_t groups = a->prefix_width != 0 ? a->n_groups : 0, mean = rows / a->n_requests;
+    p.share = (uint32_t)share, p.rows = (uint32_t)rows, p.kv_heads = (uint32_t)a->kv_heads;
+    p.whole = groups == 0 || groups >= a->n_requests || mean >= 96;
+    const uint64_t own_keys = a->own_width * a->page_tokens, prefix_keys = groups ? a->prefix_width * a->page_tokens : 0;
+    const uint64_t target = 512;  // workgroups wanted: two for each compute unit
+    for (int s = 0; s < 2; s++) {
+        p.tiles[s] = 0, p.splits[s] = 0, p.wide[s] = 0;
+        if (s == 0 && p.whole) continue;
+        const uint64_t owners = s == 0 ? groups : a->n_requests, keys = s == 0 ? prefix_keys : own_keys + (p.whole ? prefix_keys : 0);
+        p.wide[s] = rows / owners > 48;
+        const uint64_t tile_rows = p.wide[s] ? kWideRows : kNarrowRows;
+        p.tiles[s] = (uint32_t)(rows / tile_rows + owners);
+        const uint64_t real = rows / tile_rows > owners ? rows / tile_rows : owners;
+        uint64_t splits = target / (real * a->kv_heads), most = (keys + 2 * kSplitKeys - 1) / (2 * kSplitKeys);
+        if (splits > most) splits = most;
+        if (splits > 64) splits = 64;
+        p.splits[s] = splits > 1 ? (uint32_t)splits : 1;
+    }
+    p.joined = !(p.whole && p.splits[1] == 1);
+}
+
+static size_t part_bytes(const lsm_attention_t* a, const AttentionArgs& p) {
+    if (!p.joined) return 0;
+    return (size_t)(p.splits[0] + p.splits[1]) * a->n_tokens * a->q.heads * (a->head_dim * 4 + 8);
+}
+
+template <int kType, int kHead>
+static void launch(const AttentionArgs& p, uint32_t blocks, hipStream_t stream) {
+    hipLaunchKernelGGL((attention_kernel<kType, kHead>), dim3(blocks), dim3(kThreads), 0, stream, p);
+    if (!p.joined) return;
+    const uint64_t all = (uint64_t)p.n_tokens * p.share * p.kv_heads, per_block = kWaves * (kWave / (kHead / 4));
+    hipLaunchKernelGGL((join_kernel<kType, kHead>), dim3((uint32_t)((all + per_block - 1) / per_block)), dim3(kThreads), 0, stream, p);
+}
+template <int kType>
+static void launch_type(const AttentionArgs& p, uint32_t head, uint32_t blocks, hipStream_t stream) {
+    if (head == 64) launch<kType, 64>(p, blocks, stream);
+    else if (head == 128) launch<kType, 128>(p, blocks, stream);
+    else launch<kType, 256>(p, blocks, stream);
+}
+
+}  // namespace lsm
+
+using namespace lsm;
+
+extern "C" size_t lsm_prefix_attention_workspace_bytes(const lsm_attention_t* a) {
+    if (check_attention(a) != LSM_OK || a->n_tokens == 0) return 0;
+    AttentionArgs p = {};
+    plan_attention(a, p);
+    return part_bytes(a, p);
+}
+
+extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_attention(a);
+    if (rc != LSM_OK || a->n_tokens == 0) return rc;
+    AttentionArgs p = {};
+    plan_attention(a, p);
+    const size_t need = part_bytes(a, p);
+    if (need != 0 && (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uint64_t>(workspace) & 255) != 0)) return LSM_ERR_WORKSPACE;
+    const uint64_t blocks = ((uint64_t)p.tiles[0] * p.splits[0] + (uint64_t)p.tiles[1] * p.splits[1]) * p.kv_heads;
+    if (blocks >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    p.q = a->q.data, p.out = a->out.data, p.lse = a->lse, p.k = a->k_pages.data, p.v = a->v_pages.data;
+    p.q_token = a->q.token_stride, p.q_head = a->q.head_stride, p.out_token = a->out.token_stride, p.out_head = a->out.head_stride;
+    p.k_page = a->k_pages.page_stride, p.k_token = a->k_pages.token_stride, p.k_head = a->k_pages.head_stride;
+    p.v_page = a->v_pages.page_stride, p.v_token = a->v_pages.token_stride, p.v_head = a->v_pages.head_stride;
+    p.group_offsets = a->group_offsets, p.prefix_tables = a->prefix_tables, p.prefix_lens = a->prefix_lens;
+    p.q_offsets = a->q_offsets, p.own_tables = a->own_tables, p.own_lens = a->own_lens;
+    p.n_tokens = (uint32_t)a->n_tokens, p.n_requests = (uint32_t)a->n_requests, p.n_groups = (uint32_t)a->n_groups, p.n_pages = (uint32_t)a->n_pages;
+    p.page_shift = (uint32_t)__builtin_ctzll(a->page_tokens);
+    p.prefix_width = a->n_groups ? a->prefix_width : 0, p.own_width = a->own_width;
+    p.scale = a->scale * 1.44269504088896341f;
+    p.part_out = static_cast<float*>(workspace);
+    p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + (size_t)(p.splits[0] + p.splits[1]) * a->n_tokens * a->q.heads * a->head_dim * 4);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (a->dtype == LSM_BF16) launch_type<LSM_BF16>(p, a->head_dim, (uint32_t)blocks, s);
+    else launch_type<LSM_FP16>(p, a->head_dim, (uint32_t)blocks, s);
+    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
+}

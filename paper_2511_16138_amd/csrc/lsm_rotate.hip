@@ -1,0 +1,343 @@
+// lsm_rope_table, lsm_rotate_heads, lsm_kv_append: norm of each head, position rotation, and the way into the pages of the cache.
+#include <hip/hip_runtime.h>
+
+#include "lsm_cache.h"
+#include "lsm_common.h"
+
+namespace lsm {
+
+// ---------------------------------------------------------------------------------------------------------------------
+// elements
+// ---------------------------------------------------------------------------------------------------------------------
+template <int kType>
+struct Element;
+template <>
+struct Element<LSM_BF16> {
+    typedef __bf16 type;
+};
+template <>
+struct Element<LSM_FP16> {
+    typedef _Float16 type;
+};
+template <>
+struct Element<LSM_FP32> {
+    typedef float type;
+};
+
+constexpr int kEach = 8;  // elements of a lane: 16 bytes of a 16-bit type
+
+template <typename T>
+struct Lane {
+    typedef T vec __attribute__((ext_vector_type(kEach)));
+    vec v;
+};
+
+// A lane's elements as they are, in 16-byte words or one by one.
+template <typename T>
+__device__ __forceinline__ Lane<T> load_lane(const T* p, bool wide) {
+    Lane<T> r;
+    if (wide) {
+        r.v = *reinterpret_cast<const typename Lane<T>::vec*>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEach; j++) r.v[j] = p[j];
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_lane(T* p, const Lane<T>& r, bool wide) {
+    if (wide) {
+        *reinterpret_cast<typename Lane<T>::vec*>(p) = r.v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEach; j++) p[j] = r.v[j];
+    }
+}
+
+struct HeadsView {
+    const void* in;
+    void* out;
+    const void* weight;
+    int64_t in_token, in_head, out_token, out_head;  // elements
+    uint32_t heads;
+    uint32_t wide;  // bit 0: the input's rows are 16-byte aligned, bit 1: the output's
+};
+
+struct RotateArgs {
+    HeadsView part[3];  // queries, keys, values; the outputs of keys and values are pages where `slots` is given
+    const int32_t* positions;
+    const float* table;
+    const int64_t* slots;
+    int64_t page_stride[3];
+    uint64_t n_tokens, n_positions, n_slots, page_tokens;
+    uint32_t page_shift;  // log2(page_tokens), or 64 where it is no power of two
+    uint32_t head_dim, rot_dim, interleaved, weight_fp32, table_wide;
+    uint32_t slices, heads_per_slice;  // a token's heads are dealt to this many waves
+    float eps;
+};
+
+// One wave takes heads_per_slice of a token's heads (queries, keys and values counted through), 64 / kLanes of them at a time:
+// kLanes lanes of eight elements hold a head.  The rotation's cosines and sines belong to the token, so a lane reads them once
+// and keeps them for all its heads.  Bound by memory: every input is read once and every output written once.
+template <int kType, int kLanes>
+__global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
+    typedef typename Element<kType>::type T;
+    constexpr uint32_t kHeads = kWave / kLanes;  // heads at a time
+    constexpr uint32_t kAhead = 4;               // of these that are read before the first is worked on
+    const uint64_t wave = (uint64_t)blockIdx.x * (blockDim.x / kWave) + threadIdx.x / kWave;
+    const uint64_t token = wave / a.slices;
+    if (token >= a.n_tokens) return;
+    const uint32_t lane = threadIdx.x & (kWave - 1), part_lane = lane & (kLanes - 1), sub = lane / kLanes;
+    const uint32_t first = (uint32_t)(wave - token * a.slices) * a.heads_per_slice;
+    const uint32_t heads_q = a.part[0].heads, heads_qk = heads_q + a.part[1].heads, heads_all = heads_qk + a.part[2].heads;
+    const uint32_t end = min(first + a.heads_per_slice, heads_all);
+    const uint32_t e0 = part_lane * kEach;
+    const bool inside = e0 < a.head_dim;
+    const uint32_t half = a.rot_dim >> 1;
+    // the lane's angles
+    float cosine[kEach], sine[kEach];
+    const bool turns = a.table != nullptr && inside && e0 < a.rot_dim;
+#pragma unroll
+    for (int j = 0; j < kEach; j++) cosine[j] = 1.f, sine[j] = 0.f;
+    if (turns) {
+        const int32_t p = a.positions[token];
+        const bool known = p >= 0 && (uint64_t)p < a.n_positions;
+        const float* row = a.table + (known ? (uint64_t)p : 0) * a.rot_dim;
+#pragma unroll
+        for (int j = 0; j < kEach; j++) {
+            const uint32_t e = e0 + j;
+            if (e < a.rot_dim) {
+                const uint32_t i = a.interleaved ? e >> 1 : (e < half ? e : e - half);
+                const float s = row[half + i];
+                cosine[j] = known ? row[i] : __builtin_nanf("");
+                sine[j] = (a.interleaved ? (e & 1) : e >= half) ? s : -s;  // a' = a cos - b sin, b' = b cos + a sin
+            }
+        }
+    }
+    // halves apart: the other element of a pair is in the lane half / kEach further, or back, where that is whole; otherwise it is read again
+    const bool by_lane = half % kEach == 0;
+    const int other = e0 < half ? (int)(lane + half / kEach) : (int)(lane - half / kEach);
+    uint64_t slot_row = 0, slot_page = 0;
+    bool kept = true;
+    if (a.slots != nullptr) {
+        const int64_t slot = a.slots[token];
+        kept = slot >= 0 && (uint64_t)slot < a.n_slots;
+        if (kept) {
+            slot_page = a.page_shift < 64 ? (uint64_t)slot >> a.page_shift : (uint64_t)slot / a.page_tokens;
+            slot_row = (uint64_t)slot - slot_page * a.page_tokens;
+        }
+    }
+    for (uint32_t at = first; at < end; at += kHeads * kAhead) {
+        Lane<T> raw[kAhead];
+        const T* from[kAhead];
+        uint32_t which[kAhead], head[kAhead];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; u++) {
+            const uint32_t h = at + u * kHeads + sub;
+            which[u] = h >= end ? 3 : h < heads_q ? 0 : h < heads_qk ? 1 : 2;
+            head[u] = h - (which[u] == 0 ? 0 : which[u] == 1 ? heads_q : heads_qk);
+            const HeadsView& v = a.part[which[u] < 3 ? which[u] : 0];
+            from[u] = static_cast<const T*>(v.in) + (int64_t)token * v.in_token + (int64_t)head[u] * v.in_head + e0;
+            if (which[u] < 3 && inside) {
+                raw[u] = load_lane<T>(from[u], v.wide & 1);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kEach; j++) raw[u].v[j] = (T)0.f;
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; u++) {
+            const uint32_t w = which[u];
+            const HeadsView& v = a.part[w < 3 ? w : 0];
+            Lane<T> done = raw[u];
+            float x[kEach], weight[kEach];
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < kEach; j++) x[j] = (float)raw[u].v[j], sum += x[j] * x[j];
+#pragma unroll
+            for (int off = 1; off < kLanes; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+            const bool normed = w < 2 && v.weight != nullptr;
+            const float by = normed ? 1.f / sqrtf(sum / (float)a.head_dim + a.eps) : 1.f;
+            if (normed && inside) {
+#pragma unroll
+                for (int j = 0; j < kEach; j++) weight[j] = a.weight_fp32 ? static_cast<const float*>(v.weight)[e0 + j] : (float)static_cast<const T*>(v.weight)[e0 + j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < kEach; j++) weight[j] = 1.f;
+            }
+            float y[kEach], z[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; j++) y[j] = x[j] * by * weight[j];
+            if (a.table != nullptr) {
+                if (a.interleaved) {
+#pragma unroll
+                    for (int j = 0; j < kEach; j++) z[j] = y[j ^ 1];
+                } else if (by_lane) {
+#pragma unroll
+                    for (int j = 0; j < kEach; j++) z[j] = __shfl(y[j], other, kWave);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kEach; j++) {
+                        z[j] = 0.f;
+                        const uint32_t e = e0 + j;
+                        if (w < 2 && inside && e < a.rot_dim) {
+                            const int to = e < half ? (int)half : -(int)half;
+                            const float f = !normed ? 1.f : a.weight_fp32 ? static_cast<const float*>(v.weight)[(int)e + to] : (float)static_cast<const T*>(v.weight)[(int)e + to];
+                            z[j] = (float)from[u][j + to] * by * f;
+                        }
+                    }
+                }
+            }
+            if (w < 2) {
+#pragma unroll
+                for (int j = 0; j < kEach; j++) done.v[j] = (T)(turns && e0 + j < a.rot_dim ? y[j] * cosine[j] + z[j] * sine[j] : y[j]);
+            }
+            if (w < 3 && inside) {
+                T* to = static_cast<T*>(v.out) + (int64_t)head[u] * v.out_head + e0;
+                if (w > 0 && a.slots != nullptr) {
+                    if (!kept) continue;
+                    to += (int64_t)slot_page * a.page_stride[w] + (int64_t)slot_row * v.out_token;
+                } else {
+                    to += (int64_t)token * v.out_token;
+                }
+                store_lane<T>(to, done, v.wide & 2);
+            }
+        }
+    }
+}
+
+// Angles in 64 bits: at position 10^6 one in 32 bits is off by up to 0.03.
+__global__ void __launch_bounds__(256) rope_table_kernel(float* table, uint64_t n, uint32_t half, double log_theta) {
+    const uint64_t step = (uint64_t)gridDim.x * blockDim.x;
+    for (uint64_t u = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; u < n * half; u += step) {
+        const uint64_t p = u / half;
+        const uint32_t i = (uint32_t)(u - p * half);
+        double s, c;
+        sincos((double)p * exp(-(double)i / (double)half * log_theta), &s, &c);
+        table[p * 2 * half + i] = (float)c;
+        table[p * 2 * half + half + i] = (float)s;
+    }
+}
+
+static uint32_t element_bytes(uint32_t dtype) { return dtype == LSM_FP32 ? 4 : 2; }
+
+static bool rows_aligned(const void* data, const int64_t* strides, int n, uint32_t dtype) {
+    uint64_t bits = reinterpret_cast<uint64_t>(data);
+    for (int i = 0; i < n; i++) bits |= (uint64_t)strides[i] * element_bytes(dtype);
+    return (bits & 15) == 0;
+}
+
+static int check_rotation(const lsm_rotation_t* how) {
+    if (how == nullptr) return LSM_ERR_NULL;
+    if (how->dtype > LSM_FP32 || (how->weight_dtype != how->dtype && how->weight_dtype != LSM_FP32) || how->interleaved > 1) return LSM_ERR_BAD_ARG;
+    if (how->head_dim == 0 || how->head_dim % kEach != 0 || how->head_dim > LSM_MAX_HEAD_DIM) return LSM_ERR_BAD_ARG;
+    if (how->n_tokens >= 1ull << 31 || !(how->eps >= 0.f)) return LSM_ERR_BAD_ARG;
+    if (how->table != nullptr) {
+        if (how->rot_dim == 0 || how->rot_dim % 2 != 0 || how->rot_dim > how->head_dim || how->n_positions >= 1ull << 31) return LSM_ERR_BAD_ARG;
+        if (how->n_positions == 0 && how->n_tokens != 0) return LSM_ERR_BAD_ARG;
+        if (how->positions == nullptr && how->n_tokens != 0) return LSM_ERR_NULL;
+        if ((reinterpret_cast<uint64_t>(how->table) | reinterpret_cast<uint64_t>(how->positions)) & 3) return LSM_ERR_BAD_ARG;
+    }
+    return LSM_OK;
+}
+
+constexpr uint64_t kMostHeads = 1u << 16;
+
+// One of the parts with an output of its own: queries, or keys of lsm_rotate_heads.
+static int set_heads(HeadsView& v, const lsm_rotation_t* how, const lsm_heads_t* in, const void* weight, const lsm_heads_t* out) {
+    if (in == nullptr || in->heads == 0) return LSM_OK;
+    if (out == nullptr) return LSM_ERR_NULL;
+    if (in->heads > kMostHeads || out->heads != in->heads) return LSM_ERR_BAD_ARG;
+    if (how->n_tokens != 0 && (in->data == nullptr || out->data == nullptr)) return LSM_ERR_NULL;
+    const uint64_t mask = element_bytes(how->dtype) - 1;
+    if ((reinterpret_cast<uint64_t>(in->data) | reinterpret_cast<uint64_t>(out->data)) & mask) return LSM_ERR_BAD_ARG;
+    if (reinterpret_cast<uint64_t>(weight) & (element_bytes(how->weight_dtype) - 1)) return LSM_ERR_BAD_ARG;
+    const int64_t si[2] = {in->token_stride, in->head_stride}, so[2] = {out->token_stride, out->head_stride};
+    v = HeadsView{in->data, out->data, weight, in->token_stride, in->head_stride, out->token_stride, out->head_stride, (uint32_t)in->heads,
+                  (rows_aligned(in->data, si, 2, how->dtype) ? 1u : 0u) | (rows_aligned(out->data, so, 2, how->dtype) ? 2u : 0u)};
+    return LSM_OK;
+}
+
+// Keys or values that go to pages.
+static int set_paged(RotateArgs& a, int part, const lsm_rotation_t* how, const lsm_heads_t* in, const void* weight, const lsm_pages_t* pages) {
+    if (in == nullptr || pages == nullptr) return LSM_ERR_NULL;
+    const lsm_heads_t out = {pages->data, pages->token_stride, pages->head_stride, in->heads};
+    const int rc = set_heads(a.part[part], how, in, weight, &out);
+    if (rc != LSM_OK) return rc;
+    const int64_t so[3] = {pages->page_stride, pages->token_stride, pages->head_stride};
+    a.part[part].wide = (a.part[part].wide & 1) | (rows_aligned(pages->data, so, 3, how->dtype) ? 2u : 0u);
+    a.page_stride[part] = pages->page_stride;
+    return LSM_OK;
+}
+
+template <int kType>
+static void launch_type(const RotateArgs& a, uint32_t blocks, hipStream_t stream) {
+    if (a.head_dim <= 64) hipLaunchKernelGGL((rotate_kernel<kType, 8>), dim3(blocks), dim3(256), 0, stream, a);
+    else if (a.head_dim <= 128) hipLaunchKernelGGL((rotate_kernel<kType, 16>), dim3(blocks), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((rotate_kernel<kType, 32>), dim3(blocks), dim3(256), 0, stream, a);
+}
+
+static int launch_rotate(RotateArgs& a, const lsm_rotation_t* how, hipStream_t stream) {
+    a.positions = how->positions, a.table = how->table, a.n_positions = how->n_positions, a.n_tokens = how->n_tokens;
+    a.head_dim = how->head_dim, a.rot_dim = how->table ? how->rot_dim : 0, a.interleaved = how->interleaved;
+    a.weight_fp32 = how->weight_dtype == LSM_FP32, a.eps = how->eps;
+    const uint32_t heads = a.part[0].heads + a.part[1].heads + a.part[2].heads;
+    if (heads == 0 || a.n_tokens == 0) return LSM_OK;
+    const uint32_t lanes = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : 32, at_once = kWave / lanes, rounds = (heads + at_once - 1) / at_once;
+    // few tokens: more waves per token, down to one round of heads each
+    uint32_t slices = 1;
+    while (slices < rounds && a.n_tokens * slices < 4096) slices *= 2;
+    const uint32_t each = (rounds + slices - 1) / slices;
+    a.heads_per_slice = each * at_once;
+    a.slices = (heads + a.heads_per_slice - 1) / a.heads_per_slice;
+    const uint64_t waves = a.n_tokens * a.slices;
+    const uint64_t blocks = (waves + 3) / 4;
+    if (blocks >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (how->dtype == LSM_BF16) launch_type<LSM_BF16>(a, (uint32_t)blocks, stream);
+    else if (how->dtype == LSM_FP16) launch_type<LSM_FP16>(a, (uint32_t)blocks, stream);
+    else launch_type<LSM_FP32>(a, (uint32_t)blocks, stream);
+    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
+}
+
+}  // namespace lsm
+
+using namespace lsm;
+
+extern "C" int lsm_rope_table(float* table, uint64_t n_positions, uint32_t rot_dim, double theta, void* stream) {
+    if (rot_dim == 0 || rot_dim % 2 != 0 || rot_dim > LSM_MAX_HEAD_DIM || !(theta > 0.0) || n_positions >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (n_positions == 0) return LSM_OK;
+    if (table == nullptr) return LSM_ERR_NULL;
+    if (reinterpret_cast<uint64_t>(table) & 3) return LSM_ERR_BAD_ARG;
+    uint64_t blocks = (n_positions * (rot_dim / 2) + 255) / 256;
+    if (blocks > 8192) blocks = 8192;
+    hipLaunchKernelGGL(rope_table_kernel, dim3((uint32_t)blocks), dim3(256), 0, static_cast<hipStream_t>(stream), table, n_positions, rot_dim / 2, __builtin_log(theta));
+    return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
+}
+
+extern "C" int lsm_rotate_heads(const lsm_rotation_t* how, const lsm_heads_t* q, const void* q_weight, const lsm_heads_t* q_out,
+                                const lsm_heads_t* k, const void* k_weight, const lsm_heads_t* k_out, void* stream) {
+    int rc = check_rotation(how);
+    if (rc != LSM_OK) return rc;
+    RotateArgs a = {};
+    if ((rc = set_heads(a.part[0], how, q, q_weight, q_out)) != LSM_OK) return rc;
+    if ((rc = set_heads(a.part[1], how, k, k_weight, k_out)) != LSM_OK) return rc;
+    return launch_rotate(a, how, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int lsm_kv_append(const lsm_rotation_t* how, const lsm_heads_t* k, const void* k_weight, const lsm_heads_t* v, const int64_t* slots,
+                             const lsm_pages_t* k_pages, const lsm_pages_t* v_pages, uint64_t n_pages, uint64_t page_tokens, const lsm_heads_t* q,
+                             const void* q_weight, const lsm_heads_t* q_out, void* stream) {
+    int rc = check_rotation(how);
+    if (rc != LSM_OK) return rc;
+    RotateArgs a = {};
+    if (page_tokens == 0 || page_tokens >= 1ull << 31 || n_pages >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (slots == nullptr && how->n_tokens != 0) return LSM_ERR_NULL;
+    if (reinterpret_cast<uint64_t>(slots) & 7) return LSM_ERR_BAD_ARG;
+    if ((rc = set_heads(a.part[0], how, q, q_weight, q_out)) != LSM_OK) return rc;
+    if ((rc = set_paged(a, 1, how, k, k_weight, k_pages)) != LSM_OK) return rc;
+    if ((rc = set_paged(a, 2, how, v, nullptr, v_pages)) != LSM_OK) return rc;
+    if (k->heads != v->heads) return LSM_ERR_BAD_ARG;
+    a.slots = slots, a.page_tokens = page_tokens, a.n_slots = n_pages * page_tokens;
+    a.page_shift = (page_tokens & (page_tokens - 1)) == 0 ? (uint32_t)__builtin_ctzll(page_tokens) : 64;
+    return launch_rotate(a, how, static_cast<hipStream_t>(stream));
+}
