@@ -24,11 +24,12 @@ struct Element<LSM_FP32> {
     typedef float type;
 };
 
-constexpr int kEach = 8;  // elements of a lane: 16 bytes of a 16-bit type
+template <typename T>
+constexpr int kEach = 16 / (int)sizeof(T);  // elements of a lane: 16 bytes
 
 template <typename T>
 struct Lane {
-    typedef T vec __attribute__((ext_vector_type(kEach)));
+    typedef T vec __attribute__((ext_vector_type(kEach<T>)));
     vec v;
 };
 
@@ -40,7 +41,7 @@ __device__ __forceinline__ Lane<T> load_lane(const T* p, bool wide) {
         r.v = *reinterpret_cast<const typename Lane<T>::vec*>(p);
     } else {
 #pragma unroll
-        for (int j = 0; j < kEach; j++) r.v[j] = p[j];
+        for (int j = 0; j < kEach<T>; j++) r.v[j] = p[j];
     }
     return r;
 }
@@ -50,7 +51,7 @@ __device__ __forceinline__ void store_lane(T* p, const Lane<T>& r, bool wide) {
         *reinterpret_cast<typename Lane<T>::vec*>(p) = r.v;
     } else {
 #pragma unroll
-        for (int j = 0; j < kEach; j++) p[j] = r.v[j];
+        for (int j = 0; j < kEach<T>; j++) p[j] = r.v[j];
     }
 }
 
@@ -71,19 +72,166 @@ struct RotateArgs {
     int64_t page_stride[3];
     uint64_t n_tokens, n_positions, n_slots, page_tokens;
     uint32_t page_shift;  // log2(page_tokens), or 64 where it is no power of two
-    uint32_t head_dim, rot_dim, interleaved, weight_fp32, table_wide;
+    uint32_t head_dim, rot_dim, interleaved, weight_fp32;
     uint32_t slices, heads_per_slice;  // a token's heads are dealt to this many waves
     float eps;
 };
 
+// The rotation in its ordinary form: rows and table 16-byte aligned, and the other element of a pair in the lane itself
+// (neighbouring elements) or a whole number of lanes away (halves apart).
+//
 // One wave takes heads_per_slice of a token's heads (queries, keys and values counted through), 64 / kLanes of them at a time:
-// kLanes lanes of eight elements hold a head.  The rotation's cosines and sines belong to the token, so a lane reads them once
-// and keeps them for all its heads.  Bound by memory: every input is read once and every output written once.
-template <int kType, int kLanes>
+// kLanes lanes of 16 bytes hold a head.  The angles belong to the token and the weights to all, so a lane reads them once and keeps
+// them for all its heads; four heads' loads are under way before the first is worked on.  Bound by memory: every input is
+// read once and every output written once.
+template <int kType, int kLanes, bool kInterleaved>
 __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
     typedef typename Element<kType>::type T;
+    constexpr int E = kEach<T>;
     constexpr uint32_t kHeads = kWave / kLanes;  // heads at a time
     constexpr uint32_t kAhead = 4;               // of these that are read before the first is worked on
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * (blockDim.x / kWave) + threadIdx.x / kWave));
+    const uint32_t token = wave / a.slices;
+    if (token >= a.n_tokens) return;
+    const uint32_t lane = threadIdx.x & (kWave - 1), sub = lane / kLanes, e0 = (lane & (kLanes - 1)) * E;
+    const uint32_t first = (wave - token * a.slices) * a.heads_per_slice;
+    const uint32_t heads_q = a.part[0].heads, heads_qk = heads_q + a.part[1].heads, heads_all = heads_qk + a.part[2].heads;
+    const uint32_t end = min(first + a.heads_per_slice, heads_all);
+    const bool inside = e0 < a.head_dim, turns = e0 < a.rot_dim;
+    const uint32_t half = a.rot_dim >> 1;
+    const T* in[3];
+    T* out[3];
+    bool kept = true;
+    uint64_t page = 0, row = token;
+    if (a.slots != nullptr) {
+        const int64_t slot = a.slots[token];
+        kept = slot >= 0 && (uint64_t)slot < a.n_slots;
+        const uint64_t at = kept ? (uint64_t)slot : 0;
+        page = a.page_shift < 64 ? at >> a.page_shift : at / a.page_tokens;
+        row = at - page * a.page_tokens;
+    }
+#pragma unroll
+    for (int p = 0; p < 3; p++) {
+        in[p] = static_cast<const T*>(a.part[p].in) + (int64_t)token * a.part[p].in_token;
+        out[p] = static_cast<T*>(a.part[p].out) + (p == 0 ? (int64_t)token * a.part[p].out_token : (int64_t)page * a.page_stride[p] + (int64_t)row * a.part[p].out_token);
+    }
+    // the lane's angles: a' = a cos - b sin, b' = b cos + a sin, as own * cosine + other * sine
+    float cosine[E], sine[E];
+    if (turns) {
+        const int32_t p = a.positions[token];
+        const bool known = p >= 0 && (uint64_t)p < a.n_positions;
+        const float* angles = a.table + (known ? (uint64_t)p : 0) * a.rot_dim;
+        if (kInterleaved) {
+            typedef float few __attribute__((ext_vector_type(E / 2)));
+            const few c = *reinterpret_cast<const few*>(angles + e0 / 2), s = *reinterpret_cast<const few*>(angles + half + e0 / 2);
+#pragma unroll
+            for (int j = 0; j < E; j++) cosine[j] = c[j / 2], sine[j] = j & 1 ? s[j / 2] : -s[j / 2];
+        } else {
+            const uint32_t i = e0 < half ? e0 : e0 - half;
+#pragma unroll
+            for (int j = 0; j < E; j += 4) {
+                const float4 c = *reinterpret_cast<const float4*>(angles + i + j), s = *reinterpret_cast<const float4*>(angles + half + i + j);
+                cosine[j] = c.x, cosine[j + 1] = c.y, cosine[j + 2] = c.z, cosine[j + 3] = c.w;
+                sine[j] = s.x, sine[j + 1] = s.y, sine[j + 2] = s.z, sine[j + 3] = s.w;
+            }
+#pragma unroll
+            for (int j = 0; j < E; j++) sine[j] = e0 < half ? -sine[j] : sine[j];
+        }
+        if (!known) {
+#pragma unroll
+            for (int j = 0; j < E; j++) cosine[j] = __builtin_nanf("");
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; j++) cosine[j] = 1.f, sine[j] = 0.f;
+    }
+    float weight[2][E];
+#pragma unroll
+    for (int p = 0; p < 2; p++) {
+        const void* w = a.part[p].weight;
+        if (w != nullptr && inside) {
+            if (sizeof(T) == 4 || a.weight_fp32) {
+#pragma unroll
+                for (int j = 0; j < E; j++) weight[p][j] = static_cast<const float*>(w)[e0 + j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; j++) weight[p][j] = (float)static_cast<const T*>(w)[e0 + j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < E; j++) weight[p][j] = 1.f;
+        }
+    }
+    const bool normed[2] = {a.part[0].weight != nullptr, a.part[1].weight != nullptr};
+    const float mean_by = 1.f / (float)a.head_dim;
+    // halves apart: the lane that has the other element of each of this lane's pairs
+    const int other = turns ? (int)(e0 < half ? lane + half / E : lane - half / E) : (int)lane;
+    for (uint32_t at = first; at < end; at += kHeads * kAhead) {
+        Lane<T> raw[kAhead];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; u++) {
+            const uint32_t h = at + u * kHeads + sub;
+            if (h < end && inside) {
+                const T* from = h < heads_q ? in[0] + (int64_t)h * a.part[0].in_head
+                                : h < heads_qk ? in[1] + (int64_t)(h - heads_q) * a.part[1].in_head
+                                               : in[2] + (int64_t)(h - heads_qk) * a.part[2].in_head;
+                raw[u] = load_lane<T>(from + e0, true);
+            } else {
+#pragma unroll
+                for (int j = 0; j < E; j++) raw[u].v[j] = (T)0.f;
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; u++) {
+            if (at + u * kHeads >= end) break;
+            const uint32_t h = at + u * kHeads + sub;
+            const bool query = h < heads_q;
+            float y[E];
+#pragma unroll
+            for (int j = 0; j < E; j++) y[j] = (float)raw[u].v[j];
+            if (normed[0] || normed[1]) {
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < E; j++) sum += y[j] * y[j];
+#pragma unroll
+                for (int off = 1; off < kLanes; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+                const float by = __builtin_amdgcn_rsqf(sum * mean_by + a.eps);
+                if (query ? normed[0] : normed[1]) {
+#pragma unroll
+                    for (int j = 0; j < E; j++) y[j] *= by * (query ? weight[0][j] : weight[1][j]);
+                }
+            }
+            if (a.table != nullptr) {
+                float z[E];
+#pragma unroll
+                for (int j = 0; j < E; j++) z[j] = kInterleaved ? y[j ^ 1] : __shfl(y[j], other, kWave);
+                if (turns) {
+#pragma unroll
+                    for (int j = 0; j < E; j++) y[j] = y[j] * cosine[j] + z[j] * sine[j];
+                }
+            }
+            if (h < end && inside) {
+                Lane<T> done = raw[u];
+                if (h < heads_qk) {
+#pragma unroll
+                    for (int j = 0; j < E; j++) done.v[j] = (T)y[j];
+                }
+                T* to = query ? out[0] + (int64_t)h * a.part[0].out_head
+                        : h < heads_qk ? out[1] + (int64_t)(h - heads_q) * a.part[1].out_head
+                                       : out[2] + (int64_t)(h - heads_qk) * a.part[2].out_head;
+                if (query || kept) store_lane<T>(to + e0, done, true);
+            }
+        }
+    }
+}
+
+// The same for any alignment and any rot_dim: elements one by one where rows are not aligned, and the other element of a pair read
+// again where it is in no whole lane.
+template <int kType, int kLanes>
+__global__ void __launch_bounds__(256) rotate_any_kernel(const RotateArgs a) {
+    typedef typename Element<kType>::type T;
+    constexpr int E = kEach<T>;
+    constexpr uint32_t kHeads = kWave / kLanes, kAhead = 2;
     const uint64_t wave = (uint64_t)blockIdx.x * (blockDim.x / kWave) + threadIdx.x / kWave;
     const uint64_t token = wave / a.slices;
     if (token >= a.n_tokens) return;
@@ -91,20 +239,20 @@ __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
     const uint32_t first = (uint32_t)(wave - token * a.slices) * a.heads_per_slice;
     const uint32_t heads_q = a.part[0].heads, heads_qk = heads_q + a.part[1].heads, heads_all = heads_qk + a.part[2].heads;
     const uint32_t end = min(first + a.heads_per_slice, heads_all);
-    const uint32_t e0 = part_lane * kEach;
+    const uint32_t e0 = part_lane * E;
     const bool inside = e0 < a.head_dim;
     const uint32_t half = a.rot_dim >> 1;
     // the lane's angles
-    float cosine[kEach], sine[kEach];
+    float cosine[E], sine[E];
     const bool turns = a.table != nullptr && inside && e0 < a.rot_dim;
 #pragma unroll
-    for (int j = 0; j < kEach; j++) cosine[j] = 1.f, sine[j] = 0.f;
+    for (int j = 0; j < E; j++) cosine[j] = 1.f, sine[j] = 0.f;
     if (turns) {
         const int32_t p = a.positions[token];
         const bool known = p >= 0 && (uint64_t)p < a.n_positions;
         const float* row = a.table + (known ? (uint64_t)p : 0) * a.rot_dim;
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
+        for (int j = 0; j < E; j++) {
             const uint32_t e = e0 + j;
             if (e < a.rot_dim) {
                 const uint32_t i = a.interleaved ? e >> 1 : (e < half ? e : e - half);
@@ -114,9 +262,9 @@ __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
             }
         }
     }
-    // halves apart: the other element of a pair is in the lane half / kEach further, or back, where that is whole; otherwise it is read again
-    const bool by_lane = half % kEach == 0;
-    const int other = e0 < half ? (int)(lane + half / kEach) : (int)(lane - half / kEach);
+    // halves apart: the other element of a pair is in the lane half / E further, or back, where that is whole; otherwise it is read again
+    const bool by_lane = half % E == 0;
+    const int other = e0 < half ? (int)(lane + half / E) : (int)(lane - half / E);
     uint64_t slot_row = 0, slot_page = 0;
     bool kept = true;
     if (a.slots != nullptr) {
@@ -142,7 +290,7 @@ __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
                 raw[u] = load_lane<T>(from[u], v.wide & 1);
             } else {
 #pragma unroll
-                for (int j = 0; j < kEach; j++) raw[u].v[j] = (T)0.f;
+                for (int j = 0; j < E; j++) raw[u].v[j] = (T)0.f;
             }
         }
 #pragma unroll
@@ -150,34 +298,34 @@ __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
             const uint32_t w = which[u];
             const HeadsView& v = a.part[w < 3 ? w : 0];
             Lane<T> done = raw[u];
-            float x[kEach], weight[kEach];
+            float x[E], weight[E];
             float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < kEach; j++) x[j] = (float)raw[u].v[j], sum += x[j] * x[j];
+            for (int j = 0; j < E; j++) x[j] = (float)raw[u].v[j], sum += x[j] * x[j];
 #pragma unroll
             for (int off = 1; off < kLanes; off <<= 1) sum += __shfl_xor(sum, off, kWave);
             const bool normed = w < 2 && v.weight != nullptr;
             const float by = normed ? 1.f / sqrtf(sum / (float)a.head_dim + a.eps) : 1.f;
             if (normed && inside) {
 #pragma unroll
-                for (int j = 0; j < kEach; j++) weight[j] = a.weight_fp32 ? static_cast<const float*>(v.weight)[e0 + j] : (float)static_cast<const T*>(v.weight)[e0 + j];
+                for (int j = 0; j < E; j++) weight[j] = a.weight_fp32 ? static_cast<const float*>(v.weight)[e0 + j] : (float)static_cast<const T*>(v.weight)[e0 + j];
             } else {
 #pragma unroll
-                for (int j = 0; j < kEach; j++) weight[j] = 1.f;
+                for (int j = 0; j < E; j++) weight[j] = 1.f;
             }
-            float y[kEach], z[kEach];
+            float y[E], z[E];
 #pragma unroll
-            for (int j = 0; j < kEach; j++) y[j] = x[j] * by * weight[j];
+            for (int j = 0; j < E; j++) y[j] = x[j] * by * weight[j];
             if (a.table != nullptr) {
                 if (a.interleaved) {
 #pragma unroll
-                    for (int j = 0; j < kEach; j++) z[j] = y[j ^ 1];
+                    for (int j = 0; j < E; j++) z[j] = y[j ^ 1];
                 } else if (by_lane) {
 #pragma unroll
-                    for (int j = 0; j < kEach; j++) z[j] = __shfl(y[j], other, kWave);
+                    for (int j = 0; j < E; j++) z[j] = __shfl(y[j], other, kWave);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < kEach; j++) {
+                    for (int j = 0; j < E; j++) {
                         z[j] = 0.f;
                         const uint32_t e = e0 + j;
                         if (w < 2 && inside && e < a.rot_dim) {
@@ -190,7 +338,7 @@ __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
             }
             if (w < 2) {
 #pragma unroll
-                for (int j = 0; j < kEach; j++) done.v[j] = (T)(turns && e0 + j < a.rot_dim ? y[j] * cosine[j] + z[j] * sine[j] : y[j]);
+                for (int j = 0; j < E; j++) done.v[j] = (T)(turns && e0 + j < a.rot_dim ? y[j] * cosine[j] + z[j] * sine[j] : y[j]);
             }
             if (w < 3 && inside) {
                 T* to = static_cast<T*>(v.out) + (int64_t)head[u] * v.out_head + e0;
@@ -230,7 +378,7 @@ static bool rows_aligned(const void* data, const int64_t* strides, int n, uint32
 static int check_rotation(const lsm_rotation_t* how) {
     if (how == nullptr) return LSM_ERR_NULL;
     if (how->dtype > LSM_FP32 || (how->weight_dtype != how->dtype && how->weight_dtype != LSM_FP32) || how->interleaved > 1) return LSM_ERR_BAD_ARG;
-    if (how->head_dim == 0 || how->head_dim % kEach != 0 || how->head_dim > LSM_MAX_HEAD_DIM) return LSM_ERR_BAD_ARG;
+    if (how->head_dim == 0 || how->head_dim % 8 != 0 || how->head_dim > LSM_MAX_HEAD_DIM) return LSM_ERR_BAD_ARG;
     if (how->n_tokens >= 1ull << 31 || !(how->eps >= 0.f)) return LSM_ERR_BAD_ARG;
     if (how->table != nullptr) {
         if (how->rot_dim == 0 || how->rot_dim % 2 != 0 || how->rot_dim > how->head_dim || how->n_positions >= 1ull << 31) return LSM_ERR_BAD_ARG;
@@ -270,11 +418,22 @@ static int set_paged(RotateArgs& a, int part, const lsm_rotation_t* how, const l
     return LSM_OK;
 }
 
+template <int kType, int kLanes>
+static void launch_lanes(const RotateArgs& a, uint32_t blocks, hipStream_t stream) {
+    constexpr uint32_t each = kEach<typename Element<kType>::type>;
+    const bool halves_apart = !a.interleaved && a.rot_dim % (2 * each) == 0, neighbours = a.interleaved && a.rot_dim % each == 0;
+    bool wide = (reinterpret_cast<uint64_t>(a.table) & 15) == 0;
+    for (const HeadsView& v : a.part) wide = wide && (v.heads == 0 || v.wide == 3);
+    if (wide && halves_apart) hipLaunchKernelGGL((rotate_kernel<kType, kLanes, false>), dim3(blocks), dim3(256), 0, stream, a);
+    else if (wide && neighbours) hipLaunchKernelGGL((rotate_kernel<kType, kLanes, true>), dim3(blocks), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((rotate_any_kernel<kType, kLanes>), dim3(blocks), dim3(256), 0, stream, a);
+}
 template <int kType>
-static void launch_type(const RotateArgs& a, uint32_t blocks, hipStream_t stream) {
-    if (a.head_dim <= 64) hipLaunchKernelGGL((rotate_kernel<kType, 8>), dim3(blocks), dim3(256), 0, stream, a);
-    else if (a.head_dim <= 128) hipLaunchKernelGGL((rotate_kernel<kType, 16>), dim3(blocks), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((rotate_kernel<kType, 32>), dim3(blocks), dim3(256), 0, stream, a);
+static void launch_type(const RotateArgs& a, uint32_t lanes, uint32_t blocks, hipStream_t stream) {
+    if (lanes == 8) launch_lanes<kType, 8>(a, blocks, stream);
+    else if (lanes == 16) launch_lanes<kType, 16>(a, blocks, stream);
+    else if (lanes == 32) launch_lanes<kType, 32>(a, blocks, stream);
+    else launch_lanes<kType, 64>(a, blocks, stream);
 }
 
 static int launch_rotate(RotateArgs& a, const lsm_rotation_t* how, hipStream_t stream) {
@@ -283,7 +442,9 @@ static int launch_rotate(RotateArgs& a, const lsm_rotation_t* how, hipStream_t s
     a.weight_fp32 = how->weight_dtype == LSM_FP32, a.eps = how->eps;
     const uint32_t heads = a.part[0].heads + a.part[1].heads + a.part[2].heads;
     if (heads == 0 || a.n_tokens == 0) return LSM_OK;
-    const uint32_t lanes = a.head_dim <= 64 ? 8 : a.head_dim <= 128 ? 16 : 32, at_once = kWave / lanes, rounds = (heads + at_once - 1) / at_once;
+    uint32_t lanes = 8;
+    while (lanes * 16 < a.head_dim * element_bytes(how->dtype)) lanes *= 2;
+    const uint32_t at_once = kWave / lanes, rounds = (heads + at_once - 1) / at_once;
     // few tokens: more waves per token, down to one round of heads each
     uint32_t slices = 1;
     while (slices < rounds && a.n_tokens * slices < 4096) slices *= 2;
@@ -292,10 +453,10 @@ static int launch_rotate(RotateArgs& a, const lsm_rotation_t* how, hipStream_t s
     a.slices = (heads + a.heads_per_slice - 1) / a.heads_per_slice;
     const uint64_t waves = a.n_tokens * a.slices;
     const uint64_t blocks = (waves + 3) / 4;
-    if (blocks >= 1ull << 31) return LSM_ERR_BAD_ARG;
-    if (how->dtype == LSM_BF16) launch_type<LSM_BF16>(a, (uint32_t)blocks, stream);
-    else if (how->dtype == LSM_FP16) launch_type<LSM_FP16>(a, (uint32_t)blocks, stream);
-    else launch_type<LSM_FP32>(a, (uint32_t)blocks, stream);
+    if (waves >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (how->dtype == LSM_BF16) launch_type<LSM_BF16>(a, lanes, (uint32_t)blocks, stream);
+    else if (how->dtype == LSM_FP16) launch_type<LSM_FP16>(a, lanes, (uint32_t)blocks, stream);
+    else launch_type<LSM_FP32>(a, lanes, (uint32_t)blocks, stream);
     return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
 }
 
