@@ -13,6 +13,7 @@
 namespace lsm {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 template <int kType>
@@ -21,12 +22,14 @@ template <>
 struct Half<LSM_BF16> {
     typedef __bf16 type;
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Half<LSM_FP16> {
     typedef _Float16 type;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 x2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
@@ -41,7 +44,8 @@ struct AttentionArgs {
     void* out;
     float* lse;
     const void *k, *v;
-    int64_t q_token, q_head, out_token, out_head, k_page, k_token, k_head, v_page, v_token, v_head;
+    int64_t q_token, q_head, out_token, out_head;               // elements
+    uint64_t k_page, k_token, k_head, v_page, v_token, v_head;  // bytes
     const int32_t *group_offsets, *prefix_tables, *prefix_lens, *q_offsets, *own_tables, *own_lens;
     uint32_t n_tokens, n_requests, n_groups, n_pages, page_shift, kv_heads, share, rows;
     uint64_t prefix_width, own_width;
@@ -108,6 +112,36 @@ struct Item {
     uint32_t token0, hidden;       // own keys that token t sees: t - token0 + 1 + len[1] - (new tokens), as hidden = that for t = token0, minus 1, wrapped
 };
 
+// Copies 16 bytes a lane from global memory straight into LDS: lane i's from `from` + offset to `to` + 16 i.  No register is written, so the
+// compiler, which would otherwise wait for all copies before any LDS read, need not know; whoever reads the tile waits by wait_loads.
+__device__ __forceinline__ void copy_to_lds(const char* from, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+// Until at most kLeft of this wave's vector memory operations are under way, and none of its LDS ones.
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
+}
+
+// Order of the instructions around here: LDS reads of four products ahead of the first of them, so that they do not wait for LDS one by one.
+// One of them for each of kProducts products.
+template <int kProducts>
+__device__ __forceinline__ void reads_ahead() {
+    constexpr int kAhead = 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+    for (int i = 0; i < kProducts - kAhead; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+}
+
+// A score that exceeds the maximum that weights are relative to by less than this (as an exponent of two) does not move it: weights are
+// at most 2^8 then, far from the end of either type, and the accumulators need not be scaled for every new maximum.
+constexpr float kSlack = 8.f;
+
 // A team of kTeam waves goes over tiles of kKeys keys: copies them through LDS and multiplies.  kHead = head_dim.
 //
 // Scores are computed transposed, keys times queries, so that a lane holds scores of one row (row = lane % 32) and the
@@ -119,11 +153,12 @@ template <int kType, int kHead, int kTeam, int kKeys>
 struct Team {
     typedef typename Half<kType>::type T;
     typedef typename Half<kType>::x8 x8;
+    typedef typename Half<kType>::x2 x2;
     static constexpr uint32_t kWords = kHead / 8;                                 // 16-byte words of a row
-    static constexpr uint32_t kLoads = kKeys * kWords / (kTeam * kWave);          // words a lane copies of the keys of a tile, and of the values
-    static constexpr uint32_t kRowsPerLoad = kTeam * kWave / kWords;
+    static constexpr uint32_t kRowsPerLoad = kWave / kWords;                      // rows that one copy of a wave brings: all of one page
+    static constexpr uint32_t kLoads = kKeys / (kRowsPerLoad * kTeam);            // copies of a wave for the keys of a tile, and for the values
     static constexpr uint32_t kBytes = kKeys * kHead * 2;                         // of a tile of keys, or of values
-    static_assert(kKeys * kWords % (kTeam * kWave) == 0 && kKeys % 32 == 0 && kKeys <= 64, "");
+    static_assert(kKeys % (kRowsPerLoad * kTeam) == 0 && kKeys % 32 == 0 && kKeys <= 64 && kRowsPerLoad <= LSM_MIN_PAGE_TOKENS, "");
 
     static __device__ __forceinline__ uint32_t key_word(uint32_t row, uint32_t word) {  // where a 16-byte word of a key's row is
         return kWords >= 16 ? word ^ (row & 15) : word ^ ((row >> 1) & 7);
@@ -135,7 +170,7 @@ struct Team {
 
     x8 query[kHead / 16];
     f32x16 acc[kHead / 32];
-    float most, sum;  // maximum of the row so far in units of the exponent of two; this lane's share of the sum
+    float most, sum;  // what the row's weights are relative to: the largest score so far, less at most kSlack; this lane's share of the sum
 
     __device__ __forceinline__ void start() {
 #pragma unroll
@@ -145,10 +180,12 @@ struct Team {
         most = -__builtin_inff(), sum = 0.f;
     }
 
-    // One tile: keys and values are in LDS.  present: which of its keys there are; limit: how many of them this lane's row may see.
-    __device__ __forceinline__ void tile(const char* keys, const char* values, uint64_t present, int32_t limit, bool masked, float scale) {
+    typedef f32x16 Scores[kKeys / 32];
+    typedef x8 Weights[kKeys / 16];
+
+    // The scores of a tile's keys, which are in LDS.
+    __device__ __forceinline__ void score(const char* keys, Scores& s) const {
         const uint32_t lane = threadIdx.x & (kWave - 1), n = lane & 31, h = lane >> 5;
-        f32x16 s[kKeys / 32];
 #pragma unroll
         for (int b = 0; b < kKeys / 32; b++) {
 #pragma unroll
@@ -160,75 +197,99 @@ struct Team {
                 s[b] = Half<kType>::mfma(k, query[c], s[b]);
             }
         }
-        if (masked) {
+        reads_ahead<kHead / 16 * (kKeys / 32)>();
+    }
+
+    // present: which of the tile's keys there are; limit: how many of them this lane's row may see.
+    static __device__ __forceinline__ void mask(Scores& s, uint64_t present, int32_t limit) {
+        const uint32_t h = (threadIdx.x & (kWave - 1)) >> 5;
 #pragma unroll
-            for (int b = 0; b < kKeys / 32; b++) {
-                const int32_t rest = limit - b * 32;
-                uint32_t see = rest <= 0 ? 0 : rest >= 32 ? ~0u : (1u << rest) - 1;
-                see = (see & (uint32_t)(present >> (b * 32))) >> (4 * h);
+        for (int b = 0; b < kKeys / 32; b++) {
+            const int32_t rest = limit - b * 32;
+            uint32_t see = rest <= 0 ? 0 : rest >= 32 ? ~0u : (1u << rest) - 1;
+            see = (see & (uint32_t)(present >> (b * 32))) >> (4 * h);
 #pragma unroll
-                for (int j = 0; j < 16; j++) s[b][j] = (see >> (8 * (j / 4) + j % 4)) & 1 ? s[b][j] : -__builtin_inff();
-            }
+            for (int j = 0; j < 16; j++) s[b][j] = (see >> (8 * (j / 4) + j % 4)) & 1 ? s[b][j] : -__builtin_inff();
         }
+    }
+
+    // Weights of the scores, and the accumulators brought to what they are relative to.
+    __device__ __forceinline__ void weights(const Scores& s, Weights& p, float scale) {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < kKeys / 32; b++)
 #pragma unroll
             for (int j = 0; j < 16; j++) top = fmaxf(top, s[b][j]);
-        top = other_half_max(top) * scale;
-        const float now = fmaxf(most, top);
-        if (__any(now > most)) {
-            const float by = now > most ? __builtin_amdgcn_exp2f(most - now) : 1.f;
+        top = other_half_max(top);
+        const bool moves = (top - most) * scale > kSlack;
+        if (__any(moves)) {
+            const float by = moves ? __builtin_amdgcn_exp2f((most - top) * scale) : 1.f;
             sum *= by;
 #pragma unroll
             for (uint32_t i = 0; i < kHead / 32; i++)
 #pragma unroll
                 for (int j = 0; j < 16; j++) acc[i][j] *= by;
-            most = now;
+            most = moves ? top : most;
         }
-        const float base = most == -__builtin_inff() ? 0.f : most;  // a row that has seen nothing: all weights 0
-        x8 p[kKeys / 16];
+        float more = 0.f;
+        const float base = most == -__builtin_inff() ? 0.f : -most * scale;  // a row that has seen nothing: all weights 0
 #pragma unroll
         for (int b = 0; b < kKeys / 32; b++)
 #pragma unroll
-            for (int j = 0; j < 16; j++) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, -base));
-                sum += e;
-                p[b * 2 + j / 8][j % 8] = (T)e;
+            for (int j = 0; j < 16; j += 2) {
+                const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j + 1], scale, base))};
+                const x2 w = __builtin_convertvector(e, x2);  // rounded to nearest, as the values are; the sum is of the weights before that
+                sum += e[0], more += e[1];
+                p[b * 2 + j / 8][j % 8] = w[0], p[b * 2 + j / 8][j % 8 + 1] = w[1];
             }
-        // values: 16 lanes read a block of 4 keys x 16 columns, lane i of them gets column i
-        const uint32_t i16 = lane & 15, column = ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
+        sum += more;
+    }
+
+    // The left operand of product i of weigh: of columns i / kSteps * 32 .. + 31 the keys i % kSteps * 16 .. + 15.  16 lanes read a block of 4 keys x 16
+    // columns, lane i of them gets column i.
+    static constexpr uint32_t kSteps = kKeys / 16, kProducts = kHead / 32 * kSteps, kAhead = 4;
+    static __device__ __forceinline__ x8 value_operand(const char* values, uint32_t i) {
+        const uint32_t lane = threadIdx.x & (kWave - 1), h = lane >> 5, i16 = lane & 15, column = ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
+        union {
+            x8 all;
+            s16x4 part[2];
+        } u;
 #pragma unroll
-        for (uint32_t d = 0; d < kHead / 32; d++) {
+        for (uint32_t j = 0; j < 2; j++) {
+            const uint32_t row = i % kSteps * 16 + 8 * j + 4 * h + (i16 >> 2), at = i / kSteps * 32 + column;
+            const char* from = values + row * kHead * 2 + value_word(row, at >> 3) * 16 + (at & 4) * 2;
+            u.part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from));
+        }
+        return u.all;
+    }
+
+    // The values, which are in LDS, by their weights.
+    __device__ __forceinline__ void weigh(const char* values, const Weights& p) {
+        x8 v[kAhead];
 #pragma unroll
-            for (uint32_t b = 0; b < kKeys / 16; b++) {
-                union {
-                    x8 all;
-                    s16x4 part[2];
-                } u;
+        for (uint32_t i = 0; i < kAhead; i++) v[i] = value_operand(values, i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (uint32_t j = 0; j < 2; j++) {
-                    const uint32_t row = b * 16 + 8 * j + 4 * h + (i16 >> 2), at = d * 32 + column;
-                    const char* from = values + row * kHead * 2 + value_word(row, at >> 3) * 16 + (at & 4) * 2;
-                    u.part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from));
-                }
-                acc[d] = Half<kType>::mfma(u.all, p[b], acc[d]);
-            }
+        for (uint32_t i = 0; i < kProducts; i++) {
+            acc[i / kSteps] = Half<kType>::mfma(v[i % kAhead], p[i % kSteps], acc[i / kSteps]);
+            if (i + kAhead < kProducts) v[i % kAhead] = value_operand(values, i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
 
-// kType, kHead as above.  A wide tile's keys are copied by all waves together, a narrow one's by each wave for itself.
+// A wide tile's keys are copied by all waves together, a narrow one's by each wave for itself.
 template <int kType, int kHead>
 struct Shape {
     static constexpr int kWideKeys = kHead == 256 ? 32 : 64, kNarrowKeys = kHead == 64 ? 64 : 32;
     typedef Team<kType, kHead, kWaves, kWideKeys> Wide;
     typedef Team<kType, kHead, 1, kNarrowKeys> Narrow;
-    static constexpr uint32_t kLds = Wide::kBytes * 2 > Narrow::kBytes * 2 * kWaves ? Wide::kBytes * 2 : Narrow::kBytes * 2 * kWaves;
+    static constexpr uint32_t kWideLds = Wide::kBytes * 2 * 2, kNarrowLds = Narrow::kBytes * 2 * kWaves;
+    static constexpr uint32_t kLds = kWideLds > kNarrowLds ? kWideLds : kNarrowLds;
     static constexpr uint32_t kSlicePitch = 68;  // floats between rows of a slice of 64 columns of results in LDS
-    static_assert(kWaves * 32 * kSlicePitch * 4 + kWaves * 32 * 8 <= 160 * 1024, "");
     static constexpr uint32_t kOutLds = kWaves * 32 * kSlicePitch * 4 + kWaves * 32 * 8;
     static constexpr uint32_t kAllLds = kLds > kOutLds ? kLds : kOutLds;
+    static_assert(kAllLds <= 160 * 1024, "");
 };
 
 template <int kType, int kHead, bool kWide>
@@ -239,10 +300,9 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
     constexpr int kTeam = kWide ? kWaves : 1, kKeys = kWide ? S::kWideKeys : S::kNarrowKeys;
     typedef Team<kType, kHead, kTeam, kKeys> X;
     constexpr uint32_t kPerUnit = kSplitKeys / kKeys;
-    const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1), n = lane & 31, h = lane >> 5;
-    const uint32_t in_team = kWide ? threadIdx.x : lane;
-    char* keys = lds + (kWide ? 0 : wave * 2 * X::kBytes);
-    char* values = keys + X::kBytes;
+    constexpr uint64_t kAllKeys = kKeys == 64 ? ~0ull : (1ull << kKeys) - 1;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = threadIdx.x & (kWave - 1), n = lane & 31, h = lane >> 5;
+    char* buffers = lds + (kWide ? 0 : wave * 2 * X::kBytes);
 
     X x;
     x.start();
@@ -263,68 +323,140 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
     }
     const int32_t sees = (int32_t)(token - w.token0 + w.hidden) + 1;  // own keys this row sees
     // tiles of this range: of the first segment, then of the second as far as any row of the tile sees
-    const uint32_t units0 = units_of(w.len[0]), last_row = w.row_end < w.row0 + (kWide ? kWideRows : kNarrowRows) ? w.row_end - 1 : w.row0 + (kWide ? kWideRows : kNarrowRows) - 1;
+    const uint32_t units0 = units_of(w.len[0]), tile_rows = kWide ? kWideRows : kNarrowRows;
+    const uint32_t last_row = w.row_end - w.row0 < tile_rows ? w.row_end - 1 : w.row0 + tile_rows - 1;
     const uint32_t first_row = w.row0 + (kWide ? wave * 32 : 0);
     const int32_t most_seen = (int32_t)(last_row / a.share - w.token0 + w.hidden) + 1;
     const int32_t least_seen = (int32_t)(first_row / a.share - w.token0 + w.hidden) + 1;  // of the rows of this wave
     const uint32_t seen = most_seen < 0 ? 0 : (uint32_t)most_seen < w.len[1] ? (uint32_t)most_seen : w.len[1];
-    const uint32_t units = units0 + units_of(seen);
+    const uint32_t units = a.n_pages == 0 ? 0 : units0 + units_of(seen);
     const uint32_t unit1 = w.unit1 < units ? w.unit1 : units;
-    const uint32_t tile_end = unit1 * kPerUnit, step = kWide ? 1 : kWaves;
+    const uint32_t tile_end = unit1 * kPerUnit, step = kWide ? 1 : kWaves, second = units0 * kPerUnit;  // tiles from `second` on are of the second segment
     uint32_t t = w.unit0 * kPerUnit + (kWide ? 0 : wave);
 
-    const T* k_head = static_cast<const T*>(a.k) + (int64_t)kv_head * a.k_head;
-    const T* v_head = static_cast<const T*>(a.v) + (int64_t)kv_head * a.v_head;
+    // The pages of the wave's next tiles, so many of each tile, a page a lane; `pages_there`: which of them there are.  One load for 64 of them, and
+    // no vector memory operations but the copies in between, which the waits below count.
     const uint32_t page_mask = (1u << a.page_shift) - 1;
-
-    // the page of key `lane` of tile t, or -1
-    auto page_of = [&](uint32_t t) -> int32_t {
-        const uint32_t seg = t >= units0 * kPerUnit ? 1 : 0;
-        const uint32_t at = (t - (seg ? units0 * kPerUnit : 0)) * kKeys + lane;
-        const uint32_t len = seg ? seen : w.len[0];
-        if (t >= tile_end || lane >= (uint32_t)kKeys || at >= len) return -1;
-        const int32_t page = w.table[seg][at >> a.page_shift];
-        return (uint32_t)page < a.n_pages ? page : -1;
+    const uint32_t shift = a.page_shift, page_log = shift >= (kKeys == 64 ? 6 : 5) ? 0 : (kKeys == 64 ? 6 : 5) - shift;  // log2 of the pages of a tile
+    int32_t pages = -1;
+    uint64_t pages_there = 0;
+    uint32_t pages_first = 0;  // the tile of lane 0
+    auto read_pages = [&](uint32_t t) {
+        const uint32_t u = t + (lane >> page_log) * step;
+        const bool own = u >= second;
+        const uint32_t at = (u - (own ? second : 0)) * kKeys + ((lane & ((1u << page_log) - 1)) << shift);
+        pages = -1;
+        if (u < tile_end && at < (own ? seen : w.len[0])) pages = (own ? w.table[1] : w.table[0])[at >> shift];
+        pages_there = __ballot((uint32_t)pages < a.n_pages);
+        pages_first = t;
     };
-    uint4 kr[X::kLoads], vr[X::kLoads];
-    auto load = [&](uint32_t t, int32_t page) {  // page: of key `lane`
-        const uint32_t seg = t >= units0 * kPerUnit ? 1 : 0;
-        const uint32_t at = (t - (seg ? units0 * kPerUnit : 0)) * kKeys;
+    auto page_lane = [&](uint32_t t) { return (kWide ? t - pages_first : (t - pages_first) / step) << page_log; };
+    auto next_pages = [&](uint32_t t) {
+        if (page_lane(t) >= kWave) read_pages(t);
+    };
+    // Which keys of tile t there are.
+    auto keys_there = [&](uint32_t t) -> uint64_t {
+        const bool own = t >= second;
+        const uint32_t at = (t - (own ? second : 0)) * kKeys, len = own ? seen : w.len[0], left = at < len ? len - at : 0;
+        const uint64_t there = pages_there >> page_lane(t), full = (1ull << (1u << page_log)) - 1;  // at most 4 pages
+        uint64_t keys = left >= (uint32_t)kKeys ? kAllKeys : (1ull << left) - 1;
+        if ((there & full) != full) {
+            for (uint32_t i = 0; i < (1u << page_log); i++)
+                if (!((there >> i) & 1)) keys &= page_log == 0 ? 0 : ~(((1ull << (page_mask + 1)) - 1) << (i << shift));
+        }
+        return keys;
+    };
+    // One copy brings rows of one page, so the page is a scalar.  Where there is none any page does: the scores of keys that are not
+    // there are masked, and their values are zeroed in LDS.
+    const uint32_t in_load = lane / X::kWords, word = lane % X::kWords;
+    auto copy = [&](uint32_t t, const void* from, uint64_t page_bytes, uint64_t token_bytes, uint64_t head_bytes, bool values, uint32_t to) {
+        const uint32_t at = ((t - (t >= second ? second : 0)) * kKeys) & page_mask, first = page_lane(t);
+        const char* base = static_cast<const char*>(from) + (uint64_t)kv_head * head_bytes + (uint64_t)at * token_bytes;
 #pragma unroll
         for (uint32_t i = 0; i < X::kLoads; i++) {
-            const uint32_t r = i * X::kRowsPerLoad + in_team / X::kWords, c = in_team % X::kWords;
-            const int32_t p = __shfl(page, (int)r, kWave);
-            const int64_t slot = (at + r) & page_mask;
-            kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-            if (p >= 0) {
-                kr[i] = load_global_u4(reinterpret_cast<const uint4*>(k_head + p * a.k_page + slot * a.k_token + c * 8));
-                vr[i] = load_global_u4(reinterpret_cast<const uint4*>(v_head + p * a.v_page + slot * a.v_token + c * 8));
+            const uint32_t r0 = (i * kTeam + (kWide ? wave : 0)) * X::kRowsPerLoad, r = r0 + in_load;
+            const uint32_t p = (uint32_t)__builtin_amdgcn_readlane(pages, (int)(first + (r0 >> shift))), held = p < a.n_pages ? p : 0;
+            copy_to_lds(base + (uint64_t)held * page_bytes + (uint64_t)(r0 & page_mask) * token_bytes,
+                        in_load * (uint32_t)token_bytes + (values ? X::value_word(r, word) : X::key_word(r, word)) * 16, to + r0 * kHead * 2);
+        }
+    };
+    auto copy_keys = [&](uint32_t t, uint32_t to) { copy(t, a.k, a.k_page, a.k_token, a.k_head, false, to); };
+    auto copy_values = [&](uint32_t t, uint32_t to) { copy(t, a.v, a.v_page, a.v_token, a.v_head, true, to); };
+    // values of keys that are not there: zeros, whatever the page holds
+    auto zero_values = [&](uint64_t present, char* values) {
+        for (uint32_t i = kWide ? threadIdx.x : lane; i < kKeys * X::kWords; i += kTeam * kWave)
+            if (!((present >> (i / X::kWords)) & 1)) *reinterpret_cast<uint4*>(values + i * 16) = make_uint4(0, 0, 0, 0);
+    };
+    auto scores_masked = [&](uint32_t t, uint64_t present, typename X::Scores& s) {
+        const bool own = t >= second;
+        const int32_t before = (int32_t)((t - second) * kKeys);
+        if (present != kAllKeys || (own && least_seen < before + kKeys)) X::mask(s, present, own ? sees - before : kKeys);
+    };
+    const uint32_t copies = lds_address(buffers);
+    if (t < tile_end) read_pages(t);
+    if (kWide) {
+        // Two buffers: a tile is asked for while the one before it is worked on.
+        if (t < tile_end) {
+            copy_keys(t, copies);
+            copy_values(t, copies + X::kBytes);
+            uint32_t buffer = 0;
+            for (; t < tile_end; t++) {
+                const uint64_t present = keys_there(t);
+                char* keys = buffers + buffer;
+                char* values = keys + X::kBytes;
+                buffer ^= 2 * X::kBytes;
+                wait_loads<0>();
+                __builtin_amdgcn_s_barrier();  // the tile is there, and everybody is done with the one before it
+                if (t + 1 < tile_end) {
+                    next_pages(t + 1);
+                    copy_keys(t + 1, copies + buffer);
+                    copy_values(t + 1, copies + buffer + X::kBytes);
+                }
+                if (present != kAllKeys) {
+                    zero_values(present, values);
+                    wait_loads<63>();
+                    __builtin_amdgcn_s_barrier();
+                }
+                typename X::Scores s;
+                typename X::Weights p;
+                x.score(keys, s);
+                scores_masked(t, present, s);
+                x.weights(s, p, a.scale);
+                x.weigh(values, p);
             }
         }
-    };
-    int32_t page = page_of(t), next_page = page_of(t + step);
-    if (t < tile_end) load(t, page);
-    for (; t < tile_end; t += step) {
-#pragma unroll
-        for (uint32_t i = 0; i < X::kLoads; i++) {
-            const uint32_t r = i * X::kRowsPerLoad + in_team / X::kWords, c = in_team % X::kWords;
-            *reinterpret_cast<uint4*>(keys + r * kHead * 2 + X::key_word(r, c) * 16) = kr[i];
-            *reinterpret_cast<uint4*>(values + r * kHead * 2 + X::value_word(r, c) * 16) = vr[i];
+    } else {
+        // One buffer: the next keys are asked for once the scores are done with these, the next values once the sums are.
+        char* keys = buffers;
+        char* values = keys + X::kBytes;
+        if (t < tile_end) {
+            copy_keys(t, copies);
+            copy_values(t, copies + X::kBytes);
+            for (; t < tile_end; t += step) {
+                const uint64_t present = keys_there(t);
+                const bool more = t + step < tile_end;
+                typename X::Scores s;
+                typename X::Weights p;
+                wait_loads<X::kLoads>();  // but for the values
+                x.score(keys, s);
+                wait_loads<63>();
+                if (more) {
+                    next_pages(t + step);
+                    copy_keys(t + step, copies);
+                }
+                scores_masked(t, present, s);
+                x.weights(s, p, a.scale);
+                if (more) wait_loads<X::kLoads>();  // but for the next keys
+                else wait_loads<0>();
+                if (present != kAllKeys) zero_values(present, values);
+                x.weigh(values, p);
+                wait_loads<63>();
+                if (more) copy_values(t + step, copies + X::kBytes);
+            }
         }
-        if (kWide) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
-        const uint64_t present = __ballot(page >= 0);
-        page = next_page;
-        if (t + step < tile_end) load(t + step, page);
-        next_page = page_of(t + 2 * step);
-        const bool second = t >= units0 * kPerUnit;
-        const int32_t limit = second ? sees - (int32_t)((t - units0 * kPerUnit) * kKeys) : kKeys;
-        const bool masked = present != (kKeys == 64 ? ~0ull : (1ull << kKeys) - 1) || (second && least_seen < (int32_t)((t - units0 * kPerUnit + 1) * kKeys));
-        x.tile(keys, values, present, limit, masked, a.scale);
-        if (kWide) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
     }
     x.sum = other_half_sum(x.sum);
+    x.most *= a.scale;
 
     // Results go through LDS, 64 columns at a time, to be written in whole rows; a narrow tile's waves are joined on the way.
     float* slices = reinterpret_cast<float*>(lds);
@@ -510,6 +642,9 @@ static int check_attention(const lsm_attention_t* a) {
     if (!aligned_rows(a->q.data, a->q.token_stride, a->q.head_stride, 0) || !aligned_rows(a->out.data, a->out.token_stride, a->out.head_stride, 0) ||
         !aligned_rows(a->k_pages.data, a->k_pages.page_stride, a->k_pages.token_stride, a->k_pages.head_stride) ||
         !aligned_rows(a->v_pages.data, a->v_pages.page_stride, a->v_pages.token_stride, a->v_pages.head_stride)) return LSM_ERR_BAD_ARG;
+    // a copy's lanes reach 16 rows from a scalar address by 32-bit offsets
+    for (const lsm_pages_t* p : {&a->k_pages, &a->v_pages})
+        if (p->page_stride < 0 || p->token_stride < 0 || p->head_stride < 0 || p->token_stride >= 1 << 26) return LSM_ERR_BAD_ARG;
     const uint64_t words = reinterpret_cast<uint64_t>(a->lse) | reinterpret_cast<uint64_t>(a->group_offsets) | reinterpret_cast<uint64_t>(a->prefix_tables) |
                            reinterpret_cast<uint64_t>(a->prefix_lens) | reinterpret_cast<uint64_t>(a->q_offsets) | reinterpret_cast<uint64_t>(a->own_tables) |
                            reinterpret_cast<uint64_t>(a->own_lens);
@@ -581,8 +716,8 @@ extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, s
     if (blocks >= 1ull << 31) return LSM_ERR_BAD_ARG;
     p.q = a->q.data, p.out = a->out.data, p.lse = a->lse, p.k = a->k_pages.data, p.v = a->v_pages.data;
     p.q_token = a->q.token_stride, p.q_head = a->q.head_stride, p.out_token = a->out.token_stride, p.out_head = a->out.head_stride;
-    p.k_page = a->k_pages.page_stride, p.k_token = a->k_pages.token_stride, p.k_head = a->k_pages.head_stride;
-    p.v_page = a->v_pages.page_stride, p.v_token = a->v_pages.token_stride, p.v_head = a->v_pages.head_stride;
+    p.k_page = (uint64_t)a->k_pages.page_stride * 2, p.k_token = (uint64_t)a->k_pages.token_stride * 2, p.k_head = (uint64_t)a->k_pages.head_stride * 2;
+    p.v_page = (uint64_t)a->v_pages.page_stride * 2, p.v_token = (uint64_t)a->v_pages.token_stride * 2, p.v_head = (uint64_t)a->v_pages.head_stride * 2;
     p.group_offsets = a->group_offsets, p.prefix_tables = a->prefix_tables, p.prefix_lens = a->prefix_lens;
     p.q_offsets = a->q_offsets, p.own_tables = a->own_tables, p.own_lens = a->own_lens;
     p.n_tokens = (uint32_t)a->n_tokens, p.n_requests = (uint32_t)a->n_requests, p.n_groups = (uint32_t)a->n_groups, p.n_pages = (uint32_t)a->n_pages;
