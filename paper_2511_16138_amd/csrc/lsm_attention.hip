@@ -114,9 +114,12 @@ struct Item {
 
 // Copies 16 bytes a lane from global memory straight into LDS: lane i's from `from` + offset to `to` + 16 i.  No register is written, so the
 // compiler, which would otherwise wait for all copies before any LDS read, need not know; whoever reads the tile waits by wait_loads.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is the compiler's own register; it keeps nothing there from one instruction to the next
 __device__ __forceinline__ void copy_to_lds(const char* from, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 // Until at most kLeft of this wave's vector memory operations are under way, and none of its LDS ones.
 template <int kLeft>
