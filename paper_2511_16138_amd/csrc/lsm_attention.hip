@@ -45,35 +45,38 @@ struct AttentionArgs {
     float* lse;
     const void *k, *v;
     int64_t q_token, q_head, out_token, out_head;               // elements
-    uint64_t k_page, k_token, k_head, v_page, v_token, v_head;  // bytes
+    uint64_t k_head, v_head;                                    // bytes
+    uint32_t k_page, k_token, v_page, v_token;
     const int32_t *group_offsets, *prefix_tables, *prefix_lens, *q_offsets, *own_tables, *own_lens;
     uint32_t n_tokens, n_requests, n_groups, n_pages, page_shift, kv_heads, share, rows;
+    uint32_t share_part;  // for divisions by share, see divide
     uint64_t prefix_width, own_width;
     float scale;  // of the exponent of two
     // The plan.  Stage 0: rows packed by group over the prefix; stage 1: rows packed by request over its own pages, or over the
     // prefix and its own pages (`whole`).
-    uint32_t whole, tiles[2], splits[2], wide[2];
+    uint32_t whole, tiles[2], splits[2], wide[2], combos[2], combos_part[2], least[2], items0;
     uint32_t joined;  // the parts are joined by another kernel
-    float* part_out;  // [split of either stage][row][head_dim]
-    float2* part_ml;  // [split of either stage][row]: maximum in units of the exponent of two, sum
+    float* part_out;  // [split of either stage][KV head][row][head_dim]
+    float2* part_ml;  // [split of either stage][KV head][row]: maximum in units of the exponent of two, sum
 };
 
-// Keys in [0, length), in ranges of at least two splitting units; how many there are.
-__device__ __forceinline__ uint32_t split_units(uint32_t units, uint32_t splits) {
-    const uint32_t each = (units + splits - 1) / splits;
-    return each < 2 ? 2 : each;
+// x / d for x < 2^31, given part_of(d): a division takes forty instructions, and a workgroup's first pass over its instructions is most of a short call.
+inline uint32_t part_of(uint32_t d) { return 0xFFFFFFFFu / d; }
+__device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d, uint32_t part) {
+    const uint32_t q = __umulhi(x, part);  // or one too small
+    return x - q * d >= d ? q + 1 : q;
 }
-__device__ __forceinline__ uint32_t real_splits(uint32_t units, uint32_t splits) {
-    const uint32_t each = split_units(units, splits);
-    return (units + each - 1) / each;
+
+// Splitting units of a range of keys.
+__device__ __forceinline__ uint32_t split_units(uint32_t units, uint32_t splits, uint32_t least) {
+    const uint32_t each = splits == 1 ? units : (units + splits - 1) / splits;
+    return each < least ? least : each;
 }
 __device__ __forceinline__ uint32_t units_of(uint32_t keys) { return (keys + kSplitKeys - 1) / kSplitKeys; }
 
 __device__ __forceinline__ uint32_t clamp_u32(int32_t v, uint64_t most) { return v < 0 ? 0 : (uint64_t)v > most ? (uint32_t)most : (uint32_t)v; }
 __device__ __forceinline__ uint32_t prefix_len(const AttentionArgs& a, uint32_t g) { return clamp_u32(a.prefix_lens[g], a.prefix_width << a.page_shift); }
-__device__ __forceinline__ uint32_t own_len(const AttentionArgs& a, uint32_t r) { return clamp_u32(a.own_lens[r], a.own_width << a.page_shift); }
 __device__ __forceinline__ uint32_t token_of_request(const AttentionArgs& a, uint32_t r) { return clamp_u32(a.q_offsets[r], a.n_tokens); }
-__device__ __forceinline__ uint32_t token_of_group(const AttentionArgs& a, uint32_t g) { return token_of_request(a, clamp_u32(a.group_offsets[g], a.n_requests)); }
 
 // The last i < n with start(i) <= x, for start(0) <= x and start not descending; every lane of the wave calls and gets it.
 template <typename F>
@@ -108,16 +111,17 @@ struct Item {
     const int32_t* table[2];       // pages of the two segments of keys: the prefix, the request's own
     uint32_t len[2];               // their lengths
     uint32_t unit0, unit1;         // splitting units of this range; the first segment has units_of(len[0]) of them
-    uint32_t part;                 // which part it leaves
+    uint64_t part;                 // the first row of its part: of this range, this KV head
     uint32_t token0, hidden;       // own keys that token t sees: t - token0 + 1 + len[1] - (new tokens), as hidden = that for t = token0, minus 1, wrapped
 };
 
-// Copies 16 bytes a lane from global memory straight into LDS: lane i's from `from` + offset to `to` + 16 i.  No register is written, so the
+// Copies 16 bytes a lane from global memory straight into LDS: lane i's from `from` + offset to `to` + kAt + 16 i.  No register is written, so the
 // compiler, which would otherwise wait for all copies before any LDS read, need not know; whoever reads the tile waits by wait_loads.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"  // m0 is the compiler's own register; it keeps nothing there from one instruction to the next
-__device__ __forceinline__ void copy_to_lds(const char* from, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to) : "memory", "m0");
+template <int kAt>
+__device__ __forceinline__ void copy_to_lds(uint64_t from, uint32_t offset, uint32_t to) {
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to), "n"(kAt) : "memory", "m0", "scc");
 }
 #pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
@@ -125,20 +129,6 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_
 template <int kLeft>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
-}
-
-// Order of the instructions around here: LDS reads of four products ahead of the first of them, so that they do not wait for LDS one by one.
-// One of them for each of kProducts products.
-template <int kProducts>
-__device__ __forceinline__ void reads_ahead() {
-    constexpr int kAhead = 4;
-    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
-#pragma unroll
-    for (int i = 0; i < kProducts - kAhead; i++) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
 
 // A score that exceeds the maximum that weights are relative to by less than this (as an exponent of two) does not move it: weights are
@@ -186,21 +176,29 @@ struct Team {
     typedef f32x16 Scores[kKeys / 32];
     typedef x8 Weights[kKeys / 16];
 
-    // The scores of a tile's keys, which are in LDS.
+    // Product i of a tile's scores: keys i % kGroups * 32 .. + 31, elements i / kGroups * 16 .. + 15.  Its left operand, from the keys in LDS:
+    static constexpr uint32_t kGroups = kKeys / 32, kScores = kHead / 16 * kGroups, kAhead = 4;
+    static __device__ __forceinline__ x8 key_operand(const char* keys, uint32_t i) {
+        const uint32_t lane = threadIdx.x & (kWave - 1), row = i % kGroups * 32 + (lane & 31), h = lane >> 5;
+        return *reinterpret_cast<const x8*>(keys + row * kHead * 2 + key_word(row, 2 * (i / kGroups) + h) * 16);
+    }
+
+    // The scores of a tile's keys.  LDS reads go four products ahead, here and below, and the scheduler leaves the order as it is written.
     __device__ __forceinline__ void score(const char* keys, Scores& s) const {
-        const uint32_t lane = threadIdx.x & (kWave - 1), n = lane & 31, h = lane >> 5;
 #pragma unroll
-        for (int b = 0; b < kKeys / 32; b++) {
+        for (uint32_t b = 0; b < kGroups; b++)
 #pragma unroll
             for (int j = 0; j < 16; j++) s[b][j] = 0.f;
-            const uint32_t row = b * 32 + n;
+        x8 k[kAhead];
 #pragma unroll
-            for (uint32_t c = 0; c < kHead / 16; c++) {
-                const x8 k = *reinterpret_cast<const x8*>(keys + row * kHead * 2 + key_word(row, 2 * c + h) * 16);
-                s[b] = Half<kType>::mfma(k, query[c], s[b]);
-            }
+        for (uint32_t i = 0; i < kAhead; i++) k[i] = key_operand(keys, i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t i = 0; i < kScores; i++) {
+            s[i % kGroups] = Half<kType>::mfma(k[i % kAhead], query[i / kGroups], s[i % kGroups]);
+            if (i + kAhead < kScores) k[i % kAhead] = key_operand(keys, i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        reads_ahead<kHead / 16 * (kKeys / 32)>();
     }
 
     // present: which of the tile's keys there are; limit: how many of them this lane's row may see.
@@ -216,13 +214,18 @@ struct Team {
         }
     }
 
-    // Weights of the scores, and the accumulators brought to what they are relative to.
-    __device__ __forceinline__ void weights(const Scores& s, Weights& p, float scale) {
+    // The largest of a lane's scores.
+    static __device__ __forceinline__ float largest(const Scores& s) {
         float top = s[0][0];
 #pragma unroll
-        for (int b = 0; b < kKeys / 32; b++)
+        for (uint32_t b = 0; b < kGroups; b++)
 #pragma unroll
             for (int j = 0; j < 16; j++) top = fmaxf(top, s[b][j]);
+        return top;
+    }
+
+    // Brings the accumulators to what the next weights are relative to, given the lane's largest score; the addend of the weights' exponents.
+    __device__ __forceinline__ float rebase(float top, float scale) {
         top = other_half_max(top);
         const bool moves = (top - most) * scale > kSlack;
         if (__any(moves)) {
@@ -234,23 +237,52 @@ struct Team {
                 for (int j = 0; j < 16; j++) acc[i][j] *= by;
             most = moves ? top : most;
         }
+        return most == -__builtin_inff() ? 0.f : -most * scale;  // a row that has seen nothing: all weights 0
+    }
+
+    // Weights 2 i and 2 i + 1 of a lane, rounded to nearest as the values are; the sum is of the weights before that.
+    __device__ __forceinline__ void weight_pair(const Scores& s, Weights& p, uint32_t i, float scale, float base, float& more) {
+        const uint32_t b = i / 8, j = i % 8 * 2;
+        const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j + 1], scale, base))};
+        const x2 w = __builtin_convertvector(e, x2);
+        sum += e[0], more += e[1];
+        p[i / 4][j % 8] = w[0], p[i / 4][j % 8 + 1] = w[1];
+    }
+    static constexpr uint32_t kPairs = kKeys / 4;
+
+    __device__ __forceinline__ void weights(const Scores& s, Weights& p, float scale, float base) {
         float more = 0.f;
-        const float base = most == -__builtin_inff() ? 0.f : -most * scale;  // a row that has seen nothing: all weights 0
 #pragma unroll
-        for (int b = 0; b < kKeys / 32; b++)
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j + 1], scale, base))};
-                const x2 w = __builtin_convertvector(e, x2);  // rounded to nearest, as the values are; the sum is of the weights before that
-                sum += e[0], more += e[1];
-                p[b * 2 + j / 8][j % 8] = w[0], p[b * 2 + j / 8][j % 8 + 1] = w[1];
-            }
+        for (uint32_t i = 0; i < kPairs; i++) weight_pair(s, p, i, scale, base, more);
         sum += more;
     }
 
-    // The left operand of product i of weigh: of columns i / kSteps * 32 .. + 31 the keys i % kSteps * 16 .. + 15.  16 lanes read a block of 4 keys x 16
+    // The weights of a tile and, in the shadow of its products, the scores of the next one.
+    __device__ __forceinline__ void weights_and_score(const Scores& s, Weights& p, float scale, float base, const char* next_keys, Scores& next) {
+        float more = 0.f;
+#pragma unroll
+        for (uint32_t b = 0; b < kGroups; b++)
+#pragma unroll
+            for (int j = 0; j < 16; j++) next[b][j] = 0.f;
+        x8 k[kAhead];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; i++) k[i] = key_operand(next_keys, i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t i = 0; i < kScores; i++) {
+            next[i % kGroups] = Half<kType>::mfma(k[i % kAhead], query[i / kGroups], next[i % kGroups]);
+            if (i + kAhead < kScores) k[i % kAhead] = key_operand(next_keys, i + kAhead);
+#pragma unroll
+            for (uint32_t j = i * kPairs / kScores; j < (i + 1) * kPairs / kScores; j++) weight_pair(s, p, j, scale, base, more);
+            asm volatile("" : "+v"(sum), "+v"(more));  // here, in the products' shadow, and not behind them
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum += more;
+    }
+
+    // The left operand of product i of weigh: of columns i % kColumns * 32 .. + 31 the keys i / kColumns * 16 .. + 15.  16 lanes read a block of 4 keys x 16
     // columns, lane i of them gets column i.
-    static constexpr uint32_t kSteps = kKeys / 16, kProducts = kHead / 32 * kSteps, kAhead = 4;
+    static constexpr uint32_t kColumns = kHead / 32, kProducts = kColumns * (kKeys / 16);
     static __device__ __forceinline__ x8 value_operand(const char* values, uint32_t i) {
         const uint32_t lane = threadIdx.x & (kWave - 1), h = lane >> 5, i16 = lane & 15, column = ((lane >> 4) & 1) * 16 + (i16 & 3) * 4;
         union {
@@ -259,25 +291,33 @@ struct Team {
         } u;
 #pragma unroll
         for (uint32_t j = 0; j < 2; j++) {
-            const uint32_t row = i % kSteps * 16 + 8 * j + 4 * h + (i16 >> 2), at = i / kSteps * 32 + column;
+            const uint32_t row = i / kColumns * 16 + 8 * j + 4 * h + (i16 >> 2), at = i % kColumns * 32 + column;
             const char* from = values + row * kHead * 2 + value_word(row, at >> 3) * 16 + (at & 4) * 2;
             u.part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from));
         }
         return u.all;
     }
 
-    // The values, which are in LDS, by their weights.
-    __device__ __forceinline__ void weigh(const char* values, const Weights& p) {
+    // The values, which are in LDS, by their weights; kLargest: and the largest of the next tile's scores.
+    template <bool kLargest>
+    __device__ __forceinline__ float weigh(const char* values, const Weights& p, const Scores& next) {
+        float top = -__builtin_inff();
         x8 v[kAhead];
 #pragma unroll
         for (uint32_t i = 0; i < kAhead; i++) v[i] = value_operand(values, i);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (uint32_t i = 0; i < kProducts; i++) {
-            acc[i / kSteps] = Half<kType>::mfma(v[i % kAhead], p[i % kSteps], acc[i / kSteps]);
+            acc[i % kColumns] = Half<kType>::mfma(v[i % kAhead], p[i / kColumns], acc[i % kColumns]);
             if (i + kAhead < kProducts) v[i % kAhead] = value_operand(values, i + kAhead);
+            if (kLargest) {
+#pragma unroll
+                for (uint32_t j = i * kPairs / kProducts; j < (i + 1) * kPairs / kProducts; j++) top = fmaxf(fmaxf(top, next[j / 8][j % 8 * 2]), next[j / 8][j % 8 * 2 + 1]);
+                asm volatile("" : "+v"(top));
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
+        return top;
     }
 };
 
@@ -311,82 +351,90 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
     x.start();
     const uint32_t row = w.row0 + (kWide ? wave * 32 : 0) + n;
     const bool has_row = row < w.row_end;
-    const uint32_t token = row / a.share, head = kv_head * a.share + (row - token * a.share);
+    const uint32_t some_row = has_row ? row : w.row_end - 1;  // rows behind the last are copies of it, and left out in the end
+    const uint32_t token = divide(some_row, a.share, a.share_part), head = kv_head * a.share + (some_row - token * a.share);
     {
         const T* from = static_cast<const T*>(a.q) + (int64_t)token * a.q_token + (int64_t)head * a.q_head + h * 8;
 #pragma unroll
-        for (uint32_t c = 0; c < kHead / 16; c++) {
-            if (has_row) {
-                x.query[c] = *reinterpret_cast<const x8*>(from + c * 16);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; j++) x.query[c][j] = (T)0.f;
-            }
-        }
+        for (uint32_t c = 0; c < kHead / 16; c++) x.query[c] = *reinterpret_cast<const x8*>(from + c * 16);
     }
     const int32_t sees = (int32_t)(token - w.token0 + w.hidden) + 1;  // own keys this row sees
     // tiles of this range: of the first segment, then of the second as far as any row of the tile sees
     const uint32_t units0 = units_of(w.len[0]), tile_rows = kWide ? kWideRows : kNarrowRows;
     const uint32_t last_row = w.row_end - w.row0 < tile_rows ? w.row_end - 1 : w.row0 + tile_rows - 1;
     const uint32_t first_row = w.row0 + (kWide ? wave * 32 : 0);
-    const int32_t most_seen = (int32_t)(last_row / a.share - w.token0 + w.hidden) + 1;
-    const int32_t least_seen = (int32_t)(first_row / a.share - w.token0 + w.hidden) + 1;  // of the rows of this wave
+    const int32_t most_seen = (int32_t)(divide(last_row, a.share, a.share_part) - w.token0 + w.hidden) + 1;
+    const int32_t least_seen = (int32_t)(divide(first_row, a.share, a.share_part) - w.token0 + w.hidden) + 1;  // of the rows of this wave
     const uint32_t seen = most_seen < 0 ? 0 : (uint32_t)most_seen < w.len[1] ? (uint32_t)most_seen : w.len[1];
     const uint32_t units = a.n_pages == 0 ? 0 : units0 + units_of(seen);
     const uint32_t unit1 = w.unit1 < units ? w.unit1 : units;
     const uint32_t tile_end = unit1 * kPerUnit, step = kWide ? 1 : kWaves, second = units0 * kPerUnit;  // tiles from `second` on are of the second segment
     uint32_t t = w.unit0 * kPerUnit + (kWide ? 0 : wave);
 
-    // The pages of the wave's next tiles, so many of each tile, a page a lane; `pages_there`: which of them there are.  One load for 64 of them, and
-    // no vector memory operations but the copies in between, which the waits below count.
-    const uint32_t page_mask = (1u << a.page_shift) - 1;
-    const uint32_t shift = a.page_shift, page_log = shift >= (kKeys == 64 ? 6 : 5) ? 0 : (kKeys == 64 ? 6 : 5) - shift;  // log2 of the pages of a tile
-    int32_t pages = -1;
-    uint64_t pages_there = 0;
-    uint32_t pages_first = 0;  // the tile of lane 0
-    auto read_pages = [&](uint32_t t) {
-        const uint32_t u = t + (lane >> page_log) * step;
+    // Where the next tiles' tokens are, 16 of them a lane: addresses of keys and of values, and `there`: which of them have a page.  One load for 64 of these, and
+    // no vector memory operations but the copies in between, which the waits below count.  Where there is no page any does: the scores of
+    // keys that are not there are masked, and their values are zeroed in LDS.
+    constexpr uint32_t kBlocks = kKeys / 16;  // lanes of a tile
+    uint64_t k_at = 0, v_at = 0, there = 0, whole = 0;  // whole: which have a page and 16 tokens
+    uint32_t first_tile = 0;                            // of lane 0
+    auto find_pages = [&](uint32_t t) {
+        const uint32_t u = t + lane / kBlocks * step;
         const bool own = u >= second;
-        const uint32_t at = (u - (own ? second : 0)) * kKeys + ((lane & ((1u << page_log) - 1)) << shift);
-        pages = -1;
-        if (u < tile_end && at < (own ? seen : w.len[0])) pages = (own ? w.table[1] : w.table[0])[at >> shift];
-        pages_there = __ballot((uint32_t)pages < a.n_pages);
-        pages_first = t;
+        const uint32_t at = (u - (own ? second : 0)) * kKeys + lane % kBlocks * 16, len = own ? seen : w.len[0];
+        uint32_t page = ~0u;
+        if (u < tile_end && at < len) page = (uint32_t)(own ? w.table[1] : w.table[0])[at >> a.page_shift];
+        there = __ballot(page < a.n_pages), whole = __ballot(page < a.n_pages && at + 16 <= len);
+        if (page >= a.n_pages) page = 0;
+        const uint32_t in_page = at & ((1u << a.page_shift) - 1);
+        k_at = reinterpret_cast<uint64_t>(a.k) + kv_head * a.k_head + (uint64_t)page * a.k_page + in_page * a.k_token;
+        v_at = reinterpret_cast<uint64_t>(a.v) + kv_head * a.v_head + (uint64_t)page * a.v_page + in_page * a.v_token;
+        first_tile = t;
     };
-    auto page_lane = [&](uint32_t t) { return (kWide ? t - pages_first : (t - pages_first) / step) << page_log; };
-    auto next_pages = [&](uint32_t t) {
-        if (page_lane(t) >= kWave) read_pages(t);
-    };
+    auto first_lane = [&](uint32_t t) { return (kWide ? t - first_tile : (t - first_tile) / kWaves) * kBlocks; };
     // Which keys of tile t there are.
     auto keys_there = [&](uint32_t t) -> uint64_t {
+        const uint32_t first = first_lane(t), all = (1u << kBlocks) - 1;
+        if (((uint32_t)(whole >> first) & all) == all) return kAllKeys;
         const bool own = t >= second;
         const uint32_t at = (t - (own ? second : 0)) * kKeys, len = own ? seen : w.len[0], left = at < len ? len - at : 0;
-        const uint64_t there = pages_there >> page_lane(t), full = (1ull << (1u << page_log)) - 1;  // at most 4 pages
         uint64_t keys = left >= (uint32_t)kKeys ? kAllKeys : (1ull << left) - 1;
-        if ((there & full) != full) {
-            for (uint32_t i = 0; i < (1u << page_log); i++)
-                if (!((there >> i) & 1)) keys &= page_log == 0 ? 0 : ~(((1ull << (page_mask + 1)) - 1) << (i << shift));
-        }
+#pragma unroll 1
+        for (uint32_t i = 0; i < kBlocks; i++)
+            if (!((there >> (first + i)) & 1)) keys &= ~(0xFFFFull << (i * 16));
         return keys;
     };
-    // One copy brings rows of one page, so the page is a scalar.  Where there is none any page does: the scores of keys that are not
-    // there are masked, and their values are zeroed in LDS.
-    const uint32_t in_load = lane / X::kWords, word = lane % X::kWords;
-    auto copy = [&](uint32_t t, const void* from, uint64_t page_bytes, uint64_t token_bytes, uint64_t head_bytes, bool values, uint32_t to) {
-        const uint32_t at = ((t - (t >= second ? second : 0)) * kKeys) & page_mask, first = page_lane(t);
-        const char* base = static_cast<const char*>(from) + (uint64_t)kv_head * head_bytes + (uint64_t)at * token_bytes;
+    // A wave copies whole sixteens of rows, or, where there are fewer of these than waves, an equal share of one.  One copy brings rows of one page, so
+    // its address is a scalar, and what differs between its lanes does not change from tile to tile.
+    constexpr uint32_t kMyBlocks = kWide ? 1 : kBlocks, kCopies = X::kLoads / kMyBlocks, kSharers = kWide ? kWaves / kBlocks : 1;
+    static_assert(kMyBlocks * kCopies == X::kLoads && kCopies * kSharers * X::kRowsPerLoad == 16, "");
+    uint32_t k_offset[kCopies], v_offset[kCopies];
 #pragma unroll
-        for (uint32_t i = 0; i < X::kLoads; i++) {
-            const uint32_t r0 = (i * kTeam + (kWide ? wave : 0)) * X::kRowsPerLoad, r = r0 + in_load;
-            const uint32_t p = (uint32_t)__builtin_amdgcn_readlane(pages, (int)(first + (r0 >> shift))), held = p < a.n_pages ? p : 0;
-            copy_to_lds(base + (uint64_t)held * page_bytes + (uint64_t)(r0 & page_mask) * token_bytes,
-                        in_load * (uint32_t)token_bytes + (values ? X::value_word(r, word) : X::key_word(r, word)) * 16, to + r0 * kHead * 2);
+    for (uint32_t j = 0; j < kCopies; j++) {
+        const uint32_t r = (wave % kSharers * kCopies + j) * X::kRowsPerLoad + lane / X::kWords;
+        k_offset[j] = r * a.k_token + X::key_word(r, lane % X::kWords) * 16, v_offset[j] = r * a.v_token + X::value_word(r, lane % X::kWords) * 16;
+    }
+    auto copy = [&](uint32_t t, uint64_t addresses, const uint32_t (&offset)[kCopies], uint32_t to) {
+        const uint32_t first = first_lane(t) + (kWide ? wave / kSharers : 0);
+        if (kWide) to += wave * (kCopies * X::kRowsPerLoad * kHead * 2);
+#pragma unroll
+        for (uint32_t i = 0; i < kMyBlocks; i++) {
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)addresses, (int)(first + i));
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(addresses >> 32), (int)(first + i));
+            const uint64_t from = (uint64_t)hi << 32 | lo;
+            copy_to_lds<0>(from, offset[0], to + i * 16 * kHead * 2);
+            copy_to_lds<1024>(from, offset[1], to + i * 16 * kHead * 2);
+            if constexpr (kCopies >= 4) copy_to_lds<2048>(from, offset[2], to + i * 16 * kHead * 2), copy_to_lds<3072>(from, offset[3], to + i * 16 * kHead * 2);
+            if constexpr (kCopies >= 8)
+                copy_to_lds<4096>(from, offset[4], to + i * 16 * kHead * 2), copy_to_lds<5120>(from, offset[5], to + i * 16 * kHead * 2),
+                    copy_to_lds<6144>(from, offset[6], to + i * 16 * kHead * 2), copy_to_lds<7168>(from, offset[7], to + i * 16 * kHead * 2);
+            static_assert(kCopies == 2 || kCopies == 4 || kCopies == 8, "");
         }
     };
-    auto copy_keys = [&](uint32_t t, uint32_t to) { copy(t, a.k, a.k_page, a.k_token, a.k_head, false, to); };
-    auto copy_values = [&](uint32_t t, uint32_t to) { copy(t, a.v, a.v_page, a.v_token, a.v_head, true, to); };
+    auto copy_keys = [&](uint32_t t, uint32_t to) { copy(t, k_at, k_offset, to); };
+    auto copy_values = [&](uint32_t t, uint32_t to) { copy(t, v_at, v_offset, to); };
     // values of keys that are not there: zeros, whatever the page holds
     auto zero_values = [&](uint64_t present, char* values) {
+#pragma unroll 1
         for (uint32_t i = kWide ? threadIdx.x : lane; i < kKeys * X::kWords; i += kTeam * kWave)
             if (!((present >> (i / X::kWords)) & 1)) *reinterpret_cast<uint4*>(values + i * 16) = make_uint4(0, 0, 0, 0);
     };
@@ -396,36 +444,55 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
         if (present != kAllKeys || (own && least_seen < before + kKeys)) X::mask(s, present, own ? sees - before : kKeys);
     };
     const uint32_t copies = lds_address(buffers);
-    if (t < tile_end) read_pages(t);
+    if (t < tile_end) find_pages(t);
     if (kWide) {
-        // Two buffers: a tile is asked for while the one before it is worked on.
+        // Two buffers of keys and two of values.  While a tile's weights are computed the matrix cores are at the next one's scores, so keys are asked
+        // for two tiles ahead and values one.  The last tile's next scores are of whatever the buffer holds, and nobody looks at them.
         if (t < tile_end) {
             copy_keys(t, copies);
-            copy_values(t, copies + X::kBytes);
+            copy_values(t, copies + 2 * X::kBytes);
+            uint64_t present = keys_there(t), present_next = 0;
+            wait_loads<0>();
+            __builtin_amdgcn_s_barrier();
+            if (t + 1 < tile_end) {
+                if (first_lane(t + 1) >= kWave) find_pages(t + 1);
+                copy_keys(t + 1, copies + X::kBytes);
+                present_next = keys_there(t + 1);
+            }
+            typename X::Scores s, next;
+            typename X::Weights p;
+            x.score(buffers, s);
+            scores_masked(t, present, s);
+            float top = X::largest(s);
             uint32_t buffer = 0;
-            for (; t < tile_end; t++) {
-                const uint64_t present = keys_there(t);
-                char* keys = buffers + buffer;
-                char* values = keys + X::kBytes;
-                buffer ^= 2 * X::kBytes;
+            for (;;) {
+                const char* next_keys = buffers + (buffer ^ X::kBytes);
+                char* values = buffers + 2 * X::kBytes + buffer;
                 wait_loads<0>();
-                __builtin_amdgcn_s_barrier();  // the tile is there, and everybody is done with the one before it
-                if (t + 1 < tile_end) {
-                    next_pages(t + 1);
-                    copy_keys(t + 1, copies + buffer);
-                    copy_values(t + 1, copies + buffer + X::kBytes);
+                __builtin_amdgcn_s_barrier();  // these values and the next keys are there, and everybody is done with these keys and the values before
+                const bool more = t + 1 < tile_end;
+                uint64_t present_after = 0;
+                if (more) {
+                    copy_values(t + 1, copies + 2 * X::kBytes + (buffer ^ X::kBytes));
+                    if (t + 2 < tile_end) {
+                        if (first_lane(t + 2) >= kWave) find_pages(t + 2);
+                        copy_keys(t + 2, copies + buffer);
+                        present_after = keys_there(t + 2);
+                    }
                 }
                 if (present != kAllKeys) {
                     zero_values(present, values);
                     wait_loads<63>();
                     __builtin_amdgcn_s_barrier();
                 }
-                typename X::Scores s;
-                typename X::Weights p;
-                x.score(keys, s);
-                scores_masked(t, present, s);
-                x.weights(s, p, a.scale);
-                x.weigh(values, p);
+                const float base = x.rebase(top, a.scale);
+                x.weights_and_score(s, p, a.scale, base, next_keys, next);
+                if (more) scores_masked(t + 1, present_next, next);
+                top = x.template weigh<true>(values, p, next);
+                if (!more) break;
+#pragma unroll
+                for (uint32_t b = 0; b < X::kGroups; b++) s[b] = next[b];
+                t++, buffer ^= X::kBytes, present = present_next, present_next = present_after;
             }
         }
     } else {
@@ -444,15 +511,15 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
                 x.score(keys, s);
                 wait_loads<63>();
                 if (more) {
-                    next_pages(t + step);
+                    if (first_lane(t + step) >= kWave) find_pages(t + step);
                     copy_keys(t + step, copies);
                 }
                 scores_masked(t, present, s);
-                x.weights(s, p, a.scale);
+                x.weights(s, p, a.scale, x.rebase(X::largest(s), a.scale));
                 if (more) wait_loads<X::kLoads>();  // but for the next keys
                 else wait_loads<0>();
                 if (present != kAllKeys) zero_values(present, values);
-                x.weigh(values, p);
+                x.template weigh<false>(values, p, s);
                 wait_loads<63>();
                 if (more) copy_values(t + step, copies + X::kBytes);
             }
@@ -480,144 +547,205 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
         by = __builtin_amdgcn_exp2f(x.most - base);
     }
     if (!a.joined) by *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    const uint64_t place = (uint64_t)w.part * a.rows * a.kv_heads;  // rows of all KV heads: token by token, all heads of a token
     if (has_row && h == 0 && (kWide || wave == 0)) {
-        const uint64_t at = (uint64_t)token * a.share * a.kv_heads + head;
-        if (a.joined) a.part_ml[place + at] = make_float2(most, sum);
-        else if (a.lse != nullptr) a.lse[at] = sum == 0.f ? -__builtin_inff() : (most + log2f(sum)) * 0.69314718055994531f;
+        if (a.joined) a.part_ml[w.part + row] = make_float2(most, sum);
+        else if (a.lse != nullptr) a.lse[(uint64_t)token * a.share * a.kv_heads + head] = sum == 0.f ? -__builtin_inff() : (most + log2f(sum)) * 0.69314718055994531f;
+    }
+    // eight columns of up to four rows a thread
+    constexpr uint32_t kOutRows = (kWide ? kWideRows : kNarrowRows) * 8 / kThreads;
+    const uint32_t column = (threadIdx.x & 7) * 8;
+    uint64_t place[kOutRows];
+#pragma unroll
+    for (uint32_t i = 0; i < kOutRows; i++) {
+        const uint32_t r = w.row0 + i * (kThreads / 8) + threadIdx.x / 8, tok = divide(r, a.share, a.share_part);
+        place[i] = a.joined ? (w.part + r) * kHead + column : (uint64_t)tok * a.out_token + (uint64_t)(kv_head * a.share + (r - tok * a.share)) * a.out_head + column;
     }
 #pragma unroll
     for (uint32_t s = 0; s < kHead / 64; s++) {
+        if (s) __syncthreads();
 #pragma unroll
         for (uint32_t d = 0; d < 2; d++)
 #pragma unroll
             for (uint32_t j = 0; j < 4; j++) {
                 const f32x16& v = x.acc[s * 2 + d];
-                float4 o = make_float4(v[j * 4] * by, v[j * 4 + 1] * by, v[j * 4 + 2] * by, v[j * 4 + 3] * by);
+                const float4 o = make_float4(v[j * 4] * by, v[j * 4 + 1] * by, v[j * 4 + 2] * by, v[j * 4 + 3] * by);
                 *reinterpret_cast<float4*>(slices + (wave * 32 + n) * S::kSlicePitch + d * 32 + j * 8 + h * 4) = o;
             }
         __syncthreads();
-        // eight columns a thread
-        for (uint32_t u = threadIdx.x; u < (kWide ? kWideRows : kNarrowRows) * 8; u += kThreads) {
-            const uint32_t r = u >> 3, c = (u & 7) * 8;
-            if (w.row0 + r >= w.row_end) break;
-            float o[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) o[j] = slices[r * S::kSlicePitch + c + j];
+        for (uint32_t i = 0; i < kOutRows; i++) {
+            const uint32_t r = i * (kThreads / 8) + threadIdx.x / 8;
+            if (w.row0 + r >= w.row_end) break;
+            const float* from = slices + r * S::kSlicePitch + column;
+            float4 lo = *reinterpret_cast<const float4*>(from), hi = *reinterpret_cast<const float4*>(from + 4);
             if (!kWide) {
 #pragma unroll
-                for (uint32_t i = 1; i < kWaves; i++)
-#pragma unroll
-                    for (int j = 0; j < 8; j++) o[j] += slices[(i * 32 + r) * S::kSlicePitch + c + j];
+                for (uint32_t u = 1; u < kWaves; u++) {
+                    const float4 l = *reinterpret_cast<const float4*>(from + u * 32 * S::kSlicePitch), g = *reinterpret_cast<const float4*>(from + u * 32 * S::kSlicePitch + 4);
+                    lo.x += l.x, lo.y += l.y, lo.z += l.z, lo.w += l.w, hi.x += g.x, hi.y += g.y, hi.z += g.z, hi.w += g.w;
+                }
             }
-            const uint32_t tok = (w.row0 + r) / a.share, hd = kv_head * a.share + (w.row0 + r - tok * a.share);
             if (a.joined) {
-                float* to = a.part_out + (place + (uint64_t)tok * a.share * a.kv_heads + hd) * kHead + s * 64 + c;
-                *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
-                *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+                float4* to = reinterpret_cast<float4*>(a.part_out + place[i] + s * 64);
+                to[0] = lo, to[1] = hi;
             } else {
+                const float o[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
                 x8 v;
 #pragma unroll
                 for (int j = 0; j < 8; j++) v[j] = (T)o[j];
-                *reinterpret_cast<x8*>(static_cast<T*>(a.out) + (int64_t)tok * a.out_token + (int64_t)hd * a.out_head + s * 64 + c) = v;
+                *reinterpret_cast<x8*>(static_cast<T*>(a.out) + place[i] + s * 64) = v;
             }
         }
-        __syncthreads();
     }
 }
 
-template <int kType, int kHead>
+// Owner i of rows [offset(i), offset(i + 1)) has the tiles from offset(i) / (rows of a tile) + i on: at least as many as it needs, at no one else's place.
+__device__ __forceinline__ uint32_t tile_of(uint32_t token, uint32_t share, uint32_t rows_log, uint32_t owner) { return (token * share >> rows_log) + owner; }
+
+struct Owner {
+    uint32_t index, begin, end, len;  // its number, its tokens, the length of its keys
+};
+// The owner of a tile: the last one whose first tile is not behind it.  get(i) reads an owner (all of it in one go: a workgroup starts with
+// little else to do than to wait for these); every lane of the wave calls.
+template <typename F>
+__device__ __forceinline__ Owner owner_of(uint32_t n, uint32_t tile, uint32_t share, uint32_t rows_log, F get) {
+    const uint32_t lane = threadIdx.x & (kWave - 1);
+    Owner found = {0, 0, 0, 0};
+    for (uint32_t base = 0; base < n; base += kWave) {
+        const uint32_t i = base + lane;
+        const Owner o = get(i < n ? i : n - 1);
+        const uint64_t ok = __ballot(i < n && tile_of(o.begin, share, rows_log, i) <= tile);
+        const int count = __popcll(ok);
+        if (count == 0) break;
+        found.index = base + count - 1;
+        found.begin = (uint32_t)__builtin_amdgcn_readlane((int)o.begin, count - 1);
+        found.end = (uint32_t)__builtin_amdgcn_readlane((int)o.end, count - 1);
+        found.len = (uint32_t)__builtin_amdgcn_readlane((int)o.len, count - 1);
+        if (count < (int)kWave) break;
+    }
+    return found;
+}
+
+// What a launch has: both stages, or the second one alone with tiles of one kind.
+enum { kBoth = 0, kNarrowAlone = 1, kWideAlone = 2 };
+
+template <int kType, int kHead, int kStages>
 __global__ void __launch_bounds__(kThreads, kHead == 256 ? 1 : 2) attention_kernel(const AttentionArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[Shape<kType, kHead>::kAllLds];
-    uint32_t b = blockIdx.x;
-    const uint32_t items0 = a.tiles[0] * a.splits[0] * a.kv_heads, stage = b >= items0 ? 1 : 0;
-    if (stage) b -= items0;
-    const uint32_t kv_head = b % a.kv_heads, tile = b / a.kv_heads % a.tiles[stage], split = b / a.kv_heads / a.tiles[stage];
-    const bool wide = a.wide[stage] != 0;
-    const uint32_t tile_rows = wide ? kWideRows : kNarrowRows;
-    // Owner i of rows [offset(i), offset(i + 1)) has the tiles from offset(i) / tile_rows + i on: at least as many as it needs, at no one else's place
+    // The first stage's items come first: one launch has both run side by side at the seam, and items bound by the matrix cores are not slowed down
+    // by others that keep memory busy, as they are where the two take turns.
+    const uint32_t stage = kStages != kBoth || blockIdx.x >= a.items0 ? 1 : 0, item = blockIdx.x - (kStages == kBoth && stage ? a.items0 : 0);
+    // The rows of a tile change last: workgroups that read the same keys are a multiple of the heads and ranges apart, and with eight of these on one die.
+    const uint32_t combos = stage ? a.combos[1] : a.combos[0], tile = divide(item, combos, stage ? a.combos_part[1] : a.combos_part[0]), combo = item - tile * combos;
+    if (tile >= (stage ? a.tiles[1] : a.tiles[0])) return;
+    uint32_t split = 0, kv_head = combo;
+    while (kv_head >= a.kv_heads) kv_head -= a.kv_heads, split++;  // at most 64 times
+    const bool wide = kStages == kBoth ? (stage ? a.wide[1] : a.wide[0]) != 0 : kStages == kWideAlone;
+    const uint32_t rows_log = wide ? 7 : 5, tile_rows = 1u << rows_log;
+    static_assert(kWideRows == 128 && kNarrowRows == 32, "");
     Item w;
-    uint32_t owner, begin, end;
+    Owner o;
     if (stage == 0) {
-        owner = last_not_above(a.n_groups, tile, [&](uint32_t g) { return (uint64_t)token_of_group(a, g) * a.share / tile_rows + g; });
-        begin = token_of_group(a, owner), end = token_of_group(a, owner + 1);
-    } else {
-        owner = last_not_above(a.n_requests, tile, [&](uint32_t r) { return (uint64_t)token_of_request(a, r) * a.share / tile_rows + r; });
-        begin = token_of_request(a, owner), end = token_of_request(a, owner + 1);
-    }
-    const uint64_t row0 = (uint64_t)begin * a.share + (uint64_t)(tile - ((uint64_t)begin * a.share / tile_rows + owner)) * tile_rows;
-    if (end <= begin || row0 >= (uint64_t)end * a.share) return;
-    w.row0 = (uint32_t)row0;
-    w.row_end = end * a.share;
-    if (stage == 0) {
-        w.table[0] = a.prefix_tables + owner * a.prefix_width, w.len[0] = prefix_len(a, owner);
+        o = owner_of(a.n_groups, tile, a.share, rows_log, [&](uint32_t g) {
+            const int32_t r0 = a.group_offsets[g], r1 = a.group_offsets[g + 1], len = a.prefix_lens[g];
+            return Owner{g, token_of_request(a, clamp_u32(r0, a.n_requests)), token_of_request(a, clamp_u32(r1, a.n_requests)), clamp_u32(len, a.prefix_width << a.page_shift)};
+        });
+        w.table[0] = a.prefix_tables + o.index * a.prefix_width, w.len[0] = o.len;
         w.table[1] = nullptr, w.len[1] = 0;
     } else {
+        const uint32_t lane = threadIdx.x & (kWave - 1);
+        int32_t group_first = 0, group_len = 0;  // of the first 64 groups: read along with the requests
+        const bool prefixed = kStages != kBoth && a.prefix_width != 0;
+        if (prefixed) group_first = a.group_offsets[lane < a.n_groups ? lane : a.n_groups], group_len = a.prefix_lens[lane < a.n_groups ? lane : 0];
+        o = owner_of(a.n_requests, tile, a.share, rows_log, [&](uint32_t r) {
+            const int32_t t0 = a.q_offsets[r], t1 = a.q_offsets[r + 1], len = a.own_lens[r];
+            return Owner{r, clamp_u32(t0, a.n_tokens), clamp_u32(t1, a.n_tokens), clamp_u32(len, a.own_width << a.page_shift)};
+        });
         w.len[0] = 0, w.table[0] = nullptr;
-        if (a.whole && a.prefix_width != 0) {
-            const uint32_t g = group_of(a, owner);
-            w.table[0] = a.prefix_tables + g * a.prefix_width, w.len[0] = prefix_len(a, g);
+        if (prefixed) {
+            const int count = __popcll(__ballot(lane < a.n_groups && clamp_u32(group_first, a.n_requests) <= o.index));
+            uint32_t g = count > 0 ? count - 1 : 0;
+            w.len[0] = clamp_u32(__builtin_amdgcn_readlane(group_len, (int)g), a.prefix_width << a.page_shift);
+            if (count == (int)kWave && a.n_groups > kWave) g = group_of(a, o.index), w.len[0] = prefix_len(a, g);
+            w.table[0] = a.prefix_tables + g * a.prefix_width;
         }
-        w.table[1] = a.own_tables + owner * a.own_width, w.len[1] = own_len(a, owner);
+        w.table[1] = a.own_tables + o.index * a.own_width, w.len[1] = o.len;
     }
-    w.token0 = begin;
-    w.hidden = w.len[1] - (end - begin);
-    const uint32_t units = units_of(w.len[0]) + units_of(w.len[1]), each = split_units(units, a.splits[stage]);
+    const uint32_t in_owner = tile - tile_of(o.begin, a.share, rows_log, o.index);
+    if (o.end <= o.begin || in_owner >= ((o.end - o.begin) * a.share + tile_rows - 1) >> rows_log) return;
+    w.row0 = o.begin * a.share + in_owner * tile_rows;
+    w.row_end = o.end * a.share;
+    w.token0 = o.begin;
+    w.hidden = w.len[1] - (o.end - o.begin);
+    const uint32_t units = units_of(w.len[0]) + units_of(w.len[1]), each = split_units(units, stage ? a.splits[1] : a.splits[0], stage ? a.least[1] : a.least[0]);
     w.unit0 = split * each, w.unit1 = w.unit0 + each < units ? w.unit0 + each : units;
-    if (a.joined && w.unit0 >= units) return;  // not one of the ranges that there are
-    w.part = (stage ? a.splits[0] : 0) + split;
+    w.part = ((uint64_t)((stage ? a.splits[0] : 0) + split) * a.kv_heads + kv_head) * a.rows;
+    if (a.joined && w.unit0 >= units) {  // not one of the ranges that there are: its part is empty
+        if (threadIdx.x < tile_rows && w.row0 + threadIdx.x < w.row_end) a.part_ml[w.part + w.row0 + threadIdx.x] = make_float2(-__builtin_inff(), 0.f);
+        return;
+    }
     if (wide) attend<kType, kHead, true>(a, w, kv_head, lds);
     else attend<kType, kHead, false>(a, w, kv_head, lds);
 }
 
-// Joins a row's parts: those of its prefix, then those of its own pages, each in the order of the keys.  kHead / 4 lanes have a row.
+// Joins a row's parts in the order of their numbers.  kHead / 4 lanes have a row; first each has the maxima and sums of some of its parts (at most 128 in
+// all), then four columns of all of them.
 template <int kType, int kHead>
 __global__ void __launch_bounds__(kThreads) join_kernel(const AttentionArgs a) {
     typedef typename Half<kType>::type T;
-    constexpr uint32_t kLanes = kHead / 4, kRows = kWave / kLanes;  // rows of a wave
-    const uint32_t lane = threadIdx.x & (kWave - 1), heads = a.share * a.kv_heads;
-    const uint64_t all = (uint64_t)a.n_tokens * heads;
-    const uint64_t first = ((uint64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kRows;
-    if (first >= all) return;
-    uint64_t at = first + lane / kLanes;
+    typedef T x4 __attribute__((ext_vector_type(4)));
+    constexpr uint32_t kLanes = kHead / 4, kRows = kWave / kLanes, kMine = 128 / kLanes;  // lanes of a row, rows of a wave, parts of a lane
+    const uint32_t lane = threadIdx.x & (kWave - 1), in_row = lane % kLanes, parts = a.splits[0] + a.splits[1];
+    const uint64_t all = (uint64_t)a.rows * a.kv_heads;  // rows of a part, those of the first KV head first
+    uint64_t at = ((uint64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kRows + lane / kLanes;
     const bool mine = at < all;
     if (!mine) at = all - 1;
-    const uint32_t token = (uint32_t)(at / heads), head = (uint32_t)(at - (uint64_t)token * heads), c = (lane % kLanes) * 4;
-    // a wave's rows may belong to two tokens, and these to two requests
-    const uint32_t token_a = (uint32_t)(first / heads);
-    uint32_t request = last_not_above(a.n_requests, token_a, [&](uint32_t r) { return (uint64_t)token_of_request(a, r); });
-    while (request + 1 < a.n_requests && token_of_request(a, request + 1) <= token) request++;
-    uint32_t parts[2], from[2] = {0, a.splits[0]};
-    uint32_t g = 0;
-    if (a.prefix_width != 0) {
-        const uint32_t first_request = (uint32_t)__builtin_amdgcn_readfirstlane((int)request);
-        g = group_of(a, first_request);
-        while (g + 1 < a.n_groups && clamp_u32(a.group_offsets[g + 1], a.n_requests) <= request) g++;
+    float2 ml[kMine];
+    float most = -__builtin_inff();
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; i++) {
+        ml[i] = make_float2(-__builtin_inff(), 0.f);
+        if (i * kLanes + in_row < parts) ml[i] = a.part_ml[(i * kLanes + in_row) * all + at];
+        most = fmaxf(most, ml[i].x);
     }
-    const uint32_t units0 = a.prefix_width != 0 ? units_of(prefix_len(a, g)) : 0, units1 = units_of(own_len(a, request));
-    parts[0] = a.whole ? 0 : real_splits(units0, a.splits[0]);
-    parts[1] = real_splits(units1 + (a.whole ? units0 : 0), a.splits[1]);
-    float most = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (uint32_t off = 1; off < kLanes; off <<= 1) most = fmaxf(most, __shfl_xor(most, (int)off, kWave));
+    const float base = most == -__builtin_inff() ? 0.f : most;
+    float sum = 0.f;
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; i++) {
+        ml[i].x = ml[i].x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - base);
+        sum += ml[i].y * ml[i].x;
+    }
+#pragma unroll
+    for (uint32_t off = 1; off < kLanes; off <<= 1) sum += __shfl_xor(sum, (int)off, kWave);
+    const float* from = a.part_out + at * kHead + in_row * 4;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t stage = 0; stage < 2; stage++)
-        for (uint32_t i = 0; i < parts[stage]; i++) {
-            const uint64_t place = (uint64_t)(from[stage] + i) * all + at;
-            const float2 ml = a.part_ml[place];
-            const float4 v = *reinterpret_cast<const float4*>(a.part_out + place * kHead + c);
-            const float now = fmaxf(most, ml.x), base = now == -__builtin_inff() ? 0.f : now;
-            const float old_by = __builtin_amdgcn_exp2f(most - base), new_by = __builtin_amdgcn_exp2f(ml.x - base);
-            sum = sum * old_by + ml.y * new_by;
-            o.x = o.x * old_by + v.x * new_by, o.y = o.y * old_by + v.y * new_by;
-            o.z = o.z * old_by + v.z * new_by, o.w = o.w * old_by + v.w * new_by;
-            most = now;
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; i++) {
+        if (i * kLanes >= parts) break;
+        const uint32_t left = parts - i * kLanes < kLanes ? parts - i * kLanes : kLanes;
+#pragma unroll 1
+        for (uint32_t j = 0; j < left; j += 4) {
+            float4 v[4];
+            float by[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; u++) {
+                by[u] = j + u < left ? __shfl(ml[i].x, (int)(lane - in_row + j + u), kWave) : 0.f;
+                v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (by[u] != 0.f) v[u] = *reinterpret_cast<const float4*>(from + (i * kLanes + j + u) * all * kHead);  // an empty part's are not written
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 4; u++) o.x += v[u].x * by[u], o.y += v[u].y * by[u], o.z += v[u].z * by[u], o.w += v[u].w * by[u];
         }
+    }
     if (!mine) return;
+    const uint32_t kv_head = (uint32_t)at / a.rows, row = (uint32_t)at - kv_head * a.rows, token = divide(row, a.share, a.share_part), head = kv_head * a.share + (row - token * a.share);
     const float by = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    typedef T x4 __attribute__((ext_vector_type(4)));
     x4 r;
     r[0] = (T)(o.x * by), r[1] = (T)(o.y * by), r[2] = (T)(o.z * by), r[3] = (T)(o.w * by);
-    *reinterpret_cast<x4*>(static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + c) = r;
-    if (a.lse != nullptr && lane % kLanes == 0) a.lse[at] = sum == 0.f ? -__builtin_inff() : (most + log2f(sum)) * 0.69314718055994531f;
+    *reinterpret_cast<x4*>(static_cast<T*>(a.out) + (int64_t)token * a.out_token + (int64_t)head * a.out_head + in_row * 4) = r;
+    if (a.lse != nullptr && in_row == 0) a.lse[(uint64_t)token * a.share * a.kv_heads + head] = sum == 0.f ? -__builtin_inff() : (most + log2f(sum)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -645,36 +773,54 @@ static int check_attention(const lsm_attention_t* a) {
     if (!aligned_rows(a->q.data, a->q.token_stride, a->q.head_stride, 0) || !aligned_rows(a->out.data, a->out.token_stride, a->out.head_stride, 0) ||
         !aligned_rows(a->k_pages.data, a->k_pages.page_stride, a->k_pages.token_stride, a->k_pages.head_stride) ||
         !aligned_rows(a->v_pages.data, a->v_pages.page_stride, a->v_pages.token_stride, a->v_pages.head_stride)) return LSM_ERR_BAD_ARG;
-    // a copy's lanes reach 16 rows from a scalar address by 32-bit offsets
+    // the kernel has strides in bytes in 32 bits, and offsets inside a page too
     for (const lsm_pages_t* p : {&a->k_pages, &a->v_pages})
-        if (p->page_stride < 0 || p->token_stride < 0 || p->head_stride < 0 || p->token_stride >= 1 << 26) return LSM_ERR_BAD_ARG;
+        if (p->page_stride < 0 || p->token_stride < 0 || p->head_stride < 0 || p->page_stride >= 1ll << 31 || p->token_stride >= 1 << 22) return LSM_ERR_BAD_ARG;
     const uint64_t words = reinterpret_cast<uint64_t>(a->lse) | reinterpret_cast<uint64_t>(a->group_offsets) | reinterpret_cast<uint64_t>(a->prefix_tables) |
                            reinterpret_cast<uint64_t>(a->prefix_lens) | reinterpret_cast<uint64_t>(a->q_offsets) | reinterpret_cast<uint64_t>(a->own_tables) |
                            reinterpret_cast<uint64_t>(a->own_lens);
     return words & 3 ? LSM_ERR_BAD_ARG : LSM_OK;
 }
 
-// How the work is cut; from sizes that the host knows.
+// How the work is cut; from sizes that the host knows (widths of tables stand for lengths).
 static void plan_attention(const lsm_attention_t* a, AttentionArgs& p) {
     const uint64_t share = a->q.heads / a->kv_heads, rows = a->n_tokens * share;
-    const uint64_t groups = a->prefix_width != 0 ? a->n_groups : 0, mean = rows / a->n_requests;
-    p.share = (uint32_t)share, p.rows = (uint32_t)rows, p.kv_heads = (uint32_t)a->kv_heads;
-    p.whole = groups == 0 || groups >= a->n_requests || mean >= 96;
+    const uint64_t groups = a->prefix_width != 0 ? a->n_groups : 0;
     const uint64_t own_keys = a->own_width * a->page_tokens, prefix_keys = groups ? a->prefix_width * a->page_tokens : 0;
-    const uint64_t target = 512;  // workgroups wanted: two for each compute unit
+    p.share = (uint32_t)share, p.rows = (uint32_t)rows, p.kv_heads = (uint32_t)a->kv_heads;
+    // One pass over prefix and own pages for each request, where nothing is shared or a request's rows fill tiles by themselves (96 of 128), and where
+    // reading prefixes again and again is no more than 64 MB out of caches: two passes and the join of their parts cost more then (32 decodes behind
+    // 4 prefixes of 1,500, 2 KV heads: 13.8 us so and 15.7 in two stages; 200 behind 4,000, 4 KV heads, 1.7 GB: 86 and 45).
+    p.whole = groups == 0 || groups >= a->n_requests || rows / a->n_requests >= 96 ||
+              a->n_requests * a->kv_heads * (prefix_keys + own_keys) * a->head_dim * 4 <= 64ull << 20;
     for (int s = 0; s < 2; s++) {
-        p.tiles[s] = 0, p.splits[s] = 0, p.wide[s] = 0;
+        p.tiles[s] = 0, p.splits[s] = 0, p.wide[s] = 0, p.least[s] = 1;
         if (s == 0 && p.whole) continue;
         const uint64_t owners = s == 0 ? groups : a->n_requests, keys = s == 0 ? prefix_keys : own_keys + (p.whole ? prefix_keys : 0);
         p.wide[s] = rows / owners > 48;
         const uint64_t tile_rows = p.wide[s] ? kWideRows : kNarrowRows;
         p.tiles[s] = (uint32_t)(rows / tile_rows + owners);
-        const uint64_t real = rows / tile_rows > owners ? rows / tile_rows : owners;
-        uint64_t splits = target / (real * a->kv_heads), most = (keys + 2 * kSplitKeys - 1) / (2 * kSplitKeys);
+        const uint64_t items = (rows / tile_rows > owners ? rows / tile_rows : owners) * a->kv_heads;  // about so many tiles have rows
+        // Ranges of keys: enough for a workgroup on each compute unit (wide prefix tiles; more of them write more parts: 200 decodes behind 4,000
+        // 39.5 us with 256, 48 with 512), or two; narrow prefix tiles, whose time is the start and the end, 160 (64 decodes behind 8: 27.1, with 512 30).
+        uint64_t splits = (s == 1 ? 512 : p.wide[0] ? 256 : 160) / items;
+        p.least[s] = p.wide[s] ? 2 : 4;
+        if (p.whole && !p.wide[s]) {
+            // a short pass is over before its parts could be joined (4 decodes behind 512: 9.6 us in one range, 11.4 in five)
+            if (keys <= 1024) splits = 1;
+            // many ragged requests: ranges of about 1,024 keys each, so that the longest does not run on alone (96 of up to 8,000: 169 us, 204 uncut)
+            else if (items * splits >= 300 && keys > 2048) p.least[s] = 1024 / kSplitKeys, splits = keys / 1024;
+        }
+        const uint64_t most = keys / (p.least[s] * kSplitKeys);
         if (splits > most) splits = most;
         if (splits > 64) splits = 64;
         p.splits[s] = splits > 1 ? (uint32_t)splits : 1;
     }
+    p.share_part = part_of((uint32_t)share);
+    for (int s = 0; s < 2; s++) {
+        p.combos[s] = p.splits[s] * p.kv_heads, p.combos_part[s] = part_of(p.combos[s] ? p.combos[s] : 1);
+    }
+    p.items0 = p.tiles[0] * p.combos[0];
     p.joined = !(p.whole && p.splits[1] == 1);
 }
 
@@ -685,7 +831,9 @@ static size_t part_bytes(const lsm_attention_t* a, const AttentionArgs& p) {
 
 template <int kType, int kHead>
 static void launch(const AttentionArgs& p, uint32_t blocks, hipStream_t stream) {
-    hipLaunchKernelGGL((attention_kernel<kType, kHead>), dim3(blocks), dim3(kThreads), 0, stream, p);
+    if (!p.whole) hipLaunchKernelGGL((attention_kernel<kType, kHead, kBoth>), dim3(blocks), dim3(kThreads), 0, stream, p);
+    else if (p.wide[1]) hipLaunchKernelGGL((attention_kernel<kType, kHead, kWideAlone>), dim3(blocks), dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((attention_kernel<kType, kHead, kNarrowAlone>), dim3(blocks), dim3(kThreads), 0, stream, p);
     if (!p.joined) return;
     const uint64_t all = (uint64_t)p.n_tokens * p.share * p.kv_heads, per_block = kWaves * (kWave / (kHead / 4));
     hipLaunchKernelGGL((join_kernel<kType, kHead>), dim3((uint32_t)((all + per_block - 1) / per_block)), dim3(kThreads), 0, stream, p);
@@ -715,12 +863,12 @@ extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, s
     plan_attention(a, p);
     const size_t need = part_bytes(a, p);
     if (need != 0 && (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uint64_t>(workspace) & 255) != 0)) return LSM_ERR_WORKSPACE;
-    const uint64_t blocks = ((uint64_t)p.tiles[0] * p.splits[0] + (uint64_t)p.tiles[1] * p.splits[1]) * p.kv_heads;
-    if (blocks >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (((uint64_t)p.tiles[0] * p.splits[0] + (uint64_t)p.tiles[1] * p.splits[1]) * p.kv_heads >= 1ull << 30) return LSM_ERR_BAD_ARG;
+    const uint64_t blocks = (uint64_t)p.items0 + (uint64_t)p.tiles[1] * p.combos[1];
     p.q = a->q.data, p.out = a->out.data, p.lse = a->lse, p.k = a->k_pages.data, p.v = a->v_pages.data;
     p.q_token = a->q.token_stride, p.q_head = a->q.head_stride, p.out_token = a->out.token_stride, p.out_head = a->out.head_stride;
-    p.k_page = (uint64_t)a->k_pages.page_stride * 2, p.k_token = (uint64_t)a->k_pages.token_stride * 2, p.k_head = (uint64_t)a->k_pages.head_stride * 2;
-    p.v_page = (uint64_t)a->v_pages.page_stride * 2, p.v_token = (uint64_t)a->v_pages.token_stride * 2, p.v_head = (uint64_t)a->v_pages.head_stride * 2;
+    p.k_page = (uint32_t)a->k_pages.page_stride * 2, p.k_token = (uint32_t)a->k_pages.token_stride * 2, p.k_head = (uint64_t)a->k_pages.head_stride * 2;
+    p.v_page = (uint32_t)a->v_pages.page_stride * 2, p.v_token = (uint32_t)a->v_pages.token_stride * 2, p.v_head = (uint64_t)a->v_pages.head_stride * 2;
     p.group_offsets = a->group_offsets, p.prefix_tables = a->prefix_tables, p.prefix_lens = a->prefix_lens;
     p.q_offsets = a->q_offsets, p.own_tables = a->own_tables, p.own_lens = a->own_lens;
     p.n_tokens = (uint32_t)a->n_tokens, p.n_requests = (uint32_t)a->n_requests, p.n_groups = (uint32_t)a->n_groups, p.n_pages = (uint32_t)a->n_pages;
