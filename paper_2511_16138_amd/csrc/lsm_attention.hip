@@ -788,10 +788,10 @@ static void plan_attention(const lsm_attention_t* a, AttentionArgs& p) {
     const uint64_t groups = a->prefix_width != 0 ? a->n_groups : 0;
     const uint64_t own_keys = a->own_width * a->page_tokens, prefix_keys = groups ? a->prefix_width * a->page_tokens : 0;
     p.share = (uint32_t)share, p.rows = (uint32_t)rows, p.kv_heads = (uint32_t)a->kv_heads;
-    // One pass over prefix and own pages for each request, where nothing is shared or a request's rows fill tiles by themselves (96 of 128), and where
+    // One pass over prefix and own pages for each request, where nothing is shared or a request's rows fill tiles of 128 by themselves, and where
     // reading prefixes again and again is no more than 64 MB out of caches: two passes and the join of their parts cost more then (32 decodes behind
     // 4 prefixes of 1,500, 2 KV heads: 13.8 us so and 15.7 in two stages; 200 behind 4,000, 4 KV heads, 1.7 GB: 86 and 45).
-    p.whole = groups == 0 || groups >= a->n_requests || rows / a->n_requests >= 96 ||
+    p.whole = groups == 0 || groups >= a->n_requests || rows / a->n_requests >= 300 ||
               a->n_requests * a->kv_heads * (prefix_keys + own_keys) * a->head_dim * 4 <= 64ull << 20;
     for (int s = 0; s < 2; s++) {
         p.tiles[s] = 0, p.splits[s] = 0, p.wide[s] = 0, p.least[s] = 1;
@@ -801,9 +801,9 @@ static void plan_attention(const lsm_attention_t* a, AttentionArgs& p) {
         const uint64_t tile_rows = p.wide[s] ? kWideRows : kNarrowRows;
         p.tiles[s] = (uint32_t)(rows / tile_rows + owners);
         const uint64_t items = (rows / tile_rows > owners ? rows / tile_rows : owners) * a->kv_heads;  // about so many tiles have rows
-        // Ranges of keys: enough for a workgroup on each compute unit (wide prefix tiles; more of them write more parts: 200 decodes behind 4,000
-        // 39.5 us with 256, 48 with 512), or two; narrow prefix tiles, whose time is the start and the end, 160 (64 decodes behind 8: 27.1, with 512 30).
-        uint64_t splits = (s == 1 ? 512 : p.wide[0] ? 256 : 160) / items;
+        // Ranges of keys: enough for a workgroup on each compute unit (wide tiles; more of them write more parts: 200 decodes behind 4,000
+        // 39.5 us with 256, 48 with 512), or two (narrow ones); narrow prefix tiles, whose time is the start and the end, 160 (64 decodes behind 8: 27.1, with 512 30).
+        uint64_t splits = (p.wide[s] ? 256 : s == 1 ? 512 : 160) / items;
         p.least[s] = p.wide[s] ? 2 : 4;
         if (p.whole && !p.wide[s]) {
             // a short pass is over before its parts could be joined (4 decodes behind 512: 9.6 us in one range, 11.4 in five)
