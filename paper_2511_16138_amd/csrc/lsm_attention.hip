@@ -324,7 +324,7 @@ struct Team {
 // A wide tile's keys are copied by all waves together, a narrow one's by each wave for itself.
 template <int kType, int kHead>
 struct Shape {
-    static constexpr int kWideKeys = kHead == 256 ? 32 : 64, kNarrowKeys = kHead == 64 ? 64 : 32;
+    static constexpr int kWideKeys = 64, kNarrowKeys = kHead == 64 ? 64 : 32;
     typedef Team<kType, kHead, kWaves, kWideKeys> Wide;
     typedef Team<kType, kHead, 1, kNarrowKeys> Narrow;
     static constexpr uint32_t kWideLds = Wide::kBytes * 2 * 2, kNarrowLds = Narrow::kBytes * 2 * kWaves;
