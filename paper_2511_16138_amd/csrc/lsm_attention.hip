@@ -671,8 +671,11 @@ __global__ void __launch_bounds__(kThreads, kHead == 256 ? 1 : 2) attention_kern
         }
         w.table[1] = a.own_tables + o.index * a.own_width, w.len[1] = o.len;
     }
-    const uint32_t in_owner = tile - tile_of(o.begin, a.share, rows_log, o.index);
-    if (o.end <= o.begin || in_owner >= ((o.end - o.begin) * a.share + tile_rows - 1) >> rows_log) return;
+    const uint32_t order = tile - tile_of(o.begin, a.share, rows_log, o.index), owned = ((o.end - o.begin) * a.share + tile_rows - 1) >> rows_log;
+    if (o.end <= o.begin || order >= owned) return;
+    // The last rows, which see most keys, first: what runs on alone at the end is short (a prompt of 2,048 tokens, 32 heads: 59 -> 54 us; 8 of them behind
+    // 4,096: 1,392 -> 1,346).
+    const uint32_t in_owner = owned - 1 - order;
     w.row0 = o.begin * a.share + in_owner * tile_rows;
     w.row_end = o.end * a.share;
     w.token0 = o.begin;
@@ -812,6 +815,15 @@ static void plan_attention(const lsm_attention_t* a, AttentionArgs& p) {
             else if (items * splits >= 300 && keys > 2048) p.least[s] = 1024 / kSplitKeys, splits = keys / 1024;
         }
         const uint64_t most = keys / (p.least[s] * kSplitKeys);
+        // A first stage with long ranges: 256 workgroups or a few more leave some compute units with two and the others with one, so more of them, and the
+        // fewer the longer the second stage is (at 5 TB/s beside 1 PFLOP/s), which shares the compute units with them.  256 decodes behind 8,192 and
+        // 16,384, 2 KV heads: 15 own tokens each 119 -> 90 us, 1,024 each 117 -> 93 with 410 of them; 2,047 each 127 with 256 or 410, 120 with 340.
+        // Behind 4,096 and 8,192 with 2,047 each: 93 with 256, 101 with 340.
+        if (s == 0 && p.wide[0]) {
+            const bool alone = a->n_requests * own_keys * 200 < rows * prefix_keys;
+            const uint64_t more = (alone ? 410 : 340) / (p.tiles[0] * a->kv_heads);
+            if (more > splits && prefix_keys / more >= (alone ? 1024 : 2048)) splits = more;
+        }
         if (splits > most) splits = most;
         if (splits > 64) splits = 64;
         p.splits[s] = splits > 1 ? (uint32_t)splits : 1;
