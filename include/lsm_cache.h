@@ -113,8 +113,8 @@ int lsm_kv_append(const lsm_rotation_t* how, const lsm_heads_t* k, const void* k
  * With s_i = scale * (q . k_i) over those:  out = sum_i exp(s_i) v_i / sum_i exp(s_i),  lse = log sum_i exp(s_i).
  * A token that sees nothing has out = 0 and lse = -infinity.  Query head h reads KV head h / (q.heads / kv_heads).
  * Lengths are cut to [0, width * page_tokens]; the tokens of a page number outside [0, n_pages) are not seen (holes).
- * Rows behind a length, and pages that no length reaches, are never used, whatever they hold; a value that is not finite
- * makes the outputs of every token of a batch that shares its block of keys not finite, also of tokens before it.
+ * Rows behind a length, and pages that no length reaches, are never used, whatever they hold; keys and values that are not
+ * finite reach the tokens that see them and no others.
  * Offsets that descend or leave their range give an unspecified, in-bounds result.
  * dtype: LSM_BF16 or LSM_FP16; head_dim: 64, 128 or 256.  The weights of the softmax are rounded to dtype for the product
  * with the values, as the values are.  All rows 16-byte aligned: data 16-byte aligned, strides multiples of 8.

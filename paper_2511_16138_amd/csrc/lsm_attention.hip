@@ -23,6 +23,7 @@ struct Half<LSM_BF16> {
     typedef __bf16 type;
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+    static constexpr uint32_t kExponent = 0x7F80;
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
@@ -30,6 +31,7 @@ struct Half<LSM_FP16> {
     typedef _Float16 type;
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+    static constexpr uint32_t kExponent = 0x7C00;
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
@@ -298,6 +300,34 @@ struct Team {
         return u.all;
     }
 
+    // Bits 15 and 31: whether either half of a word of two values is infinite or NaN, its exponent all ones.
+    static __device__ __forceinline__ uint32_t not_finite(uint32_t two) {
+        constexpr uint32_t k = Half<kType>::kExponent;
+        return (two & (k | k << 16)) + ((0x8000 - k) | (0x8000 - k) << 16);
+    }
+
+    // Adds the values of a tile that are infinite or NaN to the rows that see their keys: there they decide the sum whatever their weight is.
+    // limit: how many of the tile's keys this lane's row sees.
+    __device__ __forceinline__ void add_not_finite(const char* values, int32_t limit) {
+        const uint32_t h = (threadIdx.x & (kWave - 1)) >> 5;
+#pragma unroll 1
+        for (uint32_t row = 0; row < kKeys; row++) {
+#pragma unroll
+            for (uint32_t i = 0; i < kColumns * 4; i++) {
+                const uint32_t column = i * 8 + h * 4;  // of the accumulators i / 4, elements i % 4 * 4 .. + 3
+                union {
+                    uint2 words;
+                    T one[4];
+                } v;
+                v.words = *reinterpret_cast<const uint2*>(values + row * kHead * 2 + value_word(row, column >> 3) * 16 + (column & 4) * 2);
+                const uint32_t bits[2] = {not_finite(v.words.x), not_finite(v.words.y)};
+#pragma unroll
+                for (uint32_t j = 0; j < 4; j++)
+                    if ((int32_t)row < limit && ((bits[j / 2] >> (j % 2 * 16 + 15)) & 1)) acc[i / 4][i % 4 * 4 + j] += (float)v.one[j];
+            }
+        }
+    }
+
     // The values, which are in LDS, by their weights; kLargest: and the largest of the next tile's scores.
     template <bool kLargest>
     __device__ __forceinline__ float weigh(const char* values, const Weights& p, const Scores& next) {
@@ -328,7 +358,7 @@ struct Shape {
     typedef Team<kType, kHead, kWaves, kWideKeys> Wide;
     typedef Team<kType, kHead, 1, kNarrowKeys> Narrow;
     static constexpr uint32_t kWideLds = Wide::kBytes * 2 * 2, kNarrowLds = Narrow::kBytes * 2 * kWaves;
-    static constexpr uint32_t kLds = kWideLds > kNarrowLds ? kWideLds : kNarrowLds;
+    static constexpr uint32_t kLds = (kWideLds > kNarrowLds ? kWideLds : kNarrowLds) + 16;  // and a word of each wave
     static constexpr uint32_t kSlicePitch = 68;  // floats between rows of a slice of 64 columns of results in LDS
     static constexpr uint32_t kOutLds = kWaves * 32 * kSlicePitch * 4 + kWaves * 32 * 8;
     static constexpr uint32_t kAllLds = kLds > kOutLds ? kLds : kOutLds;
@@ -438,6 +468,46 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
         for (uint32_t i = kWide ? threadIdx.x : lane; i < kKeys * X::kWords; i += kTeam * kWave)
             if (!((present >> (i / X::kWords)) & 1)) *reinterpret_cast<uint4*>(values + i * 16) = make_uint4(0, 0, 0, 0);
     };
+    // A tile's values where some rows of the tile do not see all keys: an infinity or NaN among them would reach these rows too, as its product with a weight
+    // of 0.  Such values are added to the rows that see them, and zeros take their places.
+    const int32_t fewest_seen = (int32_t)(divide(w.row0, a.share, a.share_part) - w.token0 + w.hidden) + 1;  // of all rows
+    auto keep_not_finite = [&](uint32_t t, char* values) {
+        const int32_t before = (int32_t)((t - second) * kKeys);
+        if (t < second || fewest_seen >= (int32_t)seen || fewest_seen >= before + kKeys) return;
+        constexpr uint32_t kMine = kKeys * X::kWords / (kTeam * kWave);
+        uint4* words = reinterpret_cast<uint4*>(values) + (kWide ? threadIdx.x : lane);
+        uint32_t any = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kMine; i++) {
+            const uint4 v = words[i * kTeam * kWave];
+            any |= X::not_finite(v.x) | X::not_finite(v.y) | X::not_finite(v.z) | X::not_finite(v.w);
+        }
+        any = __ballot((any & 0x80008000u) != 0) != 0;
+        if (kWide) {
+            uint32_t* said = reinterpret_cast<uint32_t*>(lds + S::kLds - 16);
+            if (lane == 0) said[wave] = any;
+            wait_loads<63>();
+            __builtin_amdgcn_s_barrier();
+            const uint4 all = *reinterpret_cast<const uint4*>(said);
+            any = all.x | all.y | all.z | all.w;
+        }
+        if (__builtin_amdgcn_readfirstlane((int)any) == 0) return;
+        x.add_not_finite(values, sees - before);
+        wait_loads<63>();
+        if (kWide) __builtin_amdgcn_s_barrier();
+        auto finite = [&](uint32_t& two) {
+            const uint32_t bits = X::not_finite(two);
+            two = (bits & 0x8000u ? 0 : two & 0xFFFFu) | (bits & 0x80000000u ? 0 : two & 0xFFFF0000u);
+        };
+#pragma unroll 1
+        for (uint32_t i = 0; i < kMine; i++) {
+            uint4 v = words[i * kTeam * kWave];
+            finite(v.x), finite(v.y), finite(v.z), finite(v.w);
+            words[i * kTeam * kWave] = v;
+        }
+        wait_loads<63>();
+        if (kWide) __builtin_amdgcn_s_barrier();
+    };
     auto scores_masked = [&](uint32_t t, uint64_t present, typename X::Scores& s) {
         const bool own = t >= second;
         const int32_t before = (int32_t)((t - second) * kKeys);
@@ -486,6 +556,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
                     __builtin_amdgcn_s_barrier();
                 }
                 const float base = x.rebase(top, a.scale);
+                keep_not_finite(t, values);
                 x.weights_and_score(s, p, a.scale, base, next_keys, next);
                 if (more) scores_masked(t + 1, present_next, next);
                 top = x.template weigh<true>(values, p, next);
@@ -519,6 +590,7 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
                 if (more) wait_loads<X::kLoads>();  // but for the next keys
                 else wait_loads<0>();
                 if (present != kAllKeys) zero_values(present, values);
+                keep_not_finite(t, values);
                 x.template weigh<false>(values, p, s);
                 wait_loads<63>();
                 if (more) copy_values(t + step, copies + X::kBytes);

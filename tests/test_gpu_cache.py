@@ -262,6 +262,26 @@ def test_prefix_attention_never_uses_what_no_length_reaches(lsm, garbage, q_lens
     check(lsm, *make_batch(gen, [3, 1], [70, 18], q_lens, [100, 33, 70, 61], 8, 2, 128, 32, BF16, garbage=garbage, spare=3))
 
 
+@pytest.mark.parametrize("q_lens, hq, hkv, d, dtype", [([40, 33, 5, 70], 8, 2, 128, BF16), ([130, 1, 2, 64], 4, 4, 64, FP16), ([3, 2, 1, 5], 4, 2, 128, FP16),
+                                                         ([40, 2, 90, 1], 4, 1, 256, BF16), ([9, 4, 2, 7], 2, 1, 64, BF16)])
+@pytest.mark.parametrize("in_keys", [False, True])
+def test_prefix_attention_keeps_what_is_not_finite_from_tokens_before_it(lsm, q_lens, hq, hkv, d, dtype, in_keys):
+    """Infinities and NaN in the values (NaN in the keys) of new tokens: they reach the tokens that see them, in their columns, and no others."""
+    gen = torch.Generator().manual_seed(18)
+    page = 16
+    own = [n + extra for n, extra in zip(q_lens, (37, 0, 64, 15))]
+    q, blocks, parts = make_batch(gen, [3, 1], [70, 18], q_lens, own, hq, hkv, d, page, dtype)
+    for r, n in enumerate(q_lens):
+        for i, j in enumerate(sorted({n - 1, n // 2, 1} & set(range(1, n)))):  # not the first new token, which all others see
+            at = own[r] - n + j
+            where = blocks[int(parts[4][r, at // page]), 0 if in_keys else 1, at % page, (r + i) % hkv]
+            where[(7 * j + r) % d] = math.nan if in_keys else (math.inf, math.nan, -math.inf)[i]
+    out = check(lsm, q, blocks, parts, twice=False)
+    finite = torch.isfinite(out.cpu()).all(-1).all(-1)
+    first = [sum(q_lens[:r]) for r in range(4)]
+    assert all(bool(finite[t]) for t in first) and not bool(finite.all())
+
+
 @pytest.mark.parametrize("q_lens, d", [([1, 1, 1, 1], 128), ([40, 33, 5, 70], 64), ([1, 2, 1, 3], 256)])
 def test_prefix_attention_with_holes(lsm, q_lens, d):
     """Page numbers out of range: their tokens are not seen."""
