@@ -5,6 +5,12 @@
 // A workgroup takes a tile of rows and a range of keys and goes over the keys once with a running maximum and sum; where a tile's
 // keys are dealt to several workgroups (the prefix and the own pages always are, unless rows are packed by request anyway), each
 // leaves its accumulator, maximum and sum, and a second kernel joins them in a fixed order.
+//
+// Measured, with the floor of bytes at a copy's 4.94 TB/s or of operations at a library product's 1.38 PFLOP/s:
+//   96 decodes of up to 8,000 keys, 4 KV heads of 128     180 us, 4.9 TB/s     (178: memory)
+//   64 decodes behind 8 prefixes of 512 - 1,536, 8 heads    30 us, 3.2 TB/s     (19: memory, then the way in and the join)
+//   256 decodes behind 8,192 and 16,384, 2 heads           127 us, 0.53 PFLOP/s (65: the matrix cores on the prefixes, then memory on the own pages)
+//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096        967 us, 0.98 PFLOP/s (686: matrix cores 53 % busy at 1.7 GHz, the softmax's vector instructions as long)
 #include <hip/hip_runtime.h>
 
 #include "lsm_cache.h"

@@ -83,7 +83,8 @@ struct RotateArgs {
 // One wave takes heads_per_slice of a token's heads (queries, keys and values counted through), 64 / kLanes of them at a time:
 // kLanes lanes of 16 bytes hold a head.  The angles belong to the token and the weights to all, so a lane reads them once and keeps
 // them for all its heads; four heads' loads are under way before the first is worked on.  Bound by memory: every input is
-// read once and every output written once.
+// read once and every output written once.  Measured: 8,192 tokens of 40 heads of 128 in 37 us (4.6 TB/s; a copy 4.9), 16,384 of 48 into pages in 82 (5.0), 8 tokens
+// of 34 heads in 3.5.  The loads ahead of slot, position and angles: 8,192 tokens 34 -> 40 us.
 template <int kType, int kLanes, bool kInterleaved>
 __global__ void __launch_bounds__(256) rotate_kernel(const RotateArgs a) {
     typedef typename Element<kType>::type T;

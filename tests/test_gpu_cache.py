@@ -304,6 +304,14 @@ def test_prefix_attention_of_large_and_zero_scores(lsm, scale, size):
     check(lsm, (q.float() * size).to(BF16), blocks, parts, scale=scale)
 
 
+@pytest.mark.parametrize("groups, prefix, hq", [([33, 31], [12400, 3001], 64), ([40], [8200], 64), ([30, 10], [6000, 6000], 32)])
+def test_prefix_attention_of_many_requests_behind_long_prefixes(lsm, groups, prefix, hq):
+    """Wide first stages, their keys dealt to different numbers of workgroups, beside narrow second ones."""
+    gen = torch.Generator().manual_seed(19)
+    n = sum(groups)
+    check(lsm, *make_batch(gen, groups, prefix, [1] * n, [1 + (i * 5) % 37 for i in range(n)], hq, 1, 64, 256, BF16))
+
+
 def test_prefix_attention_of_strided_tensors(lsm):
     gen = torch.Generator().manual_seed(15)
     q, blocks, parts = make_batch(gen, [2, 2], [50, 20], [1, 3, 1, 2], [40, 33, 1, 90], 8, 2, 64, 16, BF16)
