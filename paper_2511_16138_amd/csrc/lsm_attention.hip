@@ -10,7 +10,7 @@
 //   96 decodes of up to 8,000 keys, 4 KV heads of 128     180 us, 4.9 TB/s     (178: memory)
 //   64 decodes behind 8 prefixes of 512 - 1,536, 8 heads    30 us, 3.2 TB/s     (19: memory, then the way in and the join)
 //   256 decodes behind 8,192 and 16,384, 2 heads           127 us, 0.53 PFLOP/s (65: the matrix cores on the prefixes, then memory on the own pages)
-//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096        967 us, 0.98 PFLOP/s (686: matrix cores 53 % busy at 1.7 GHz, the softmax's vector instructions as long)
+//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096        967 us, 0.98 PFLOP/s (686: matrix cores 52 % busy at 1.7 GHz, the softmax's vector instructions as long)
 #include <hip/hip_runtime.h>
 
 #include "lsm_cache.h"
@@ -567,7 +567,6 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
                 if (more) scores_masked(t + 1, present_next, next);
                 top = x.template weigh<true>(values, p, next);
                 if (!more) break;
-#pragma unroll
                 for (uint32_t b = 0; b < X::kGroups; b++) s[b] = next[b];
                 t++, buffer ^= X::kBytes, present = present_next, present_next = present_after;
             }
