@@ -123,13 +123,20 @@ struct Item {
     uint32_t token0, hidden;       // own keys that token t sees: t - token0 + 1 + len[1] - (new tokens), as hidden = that for t = token0, minus 1, wrapped
 };
 
-// Copies 16 bytes a lane from global memory straight into LDS: lane i's from `from` + offset to `to` + kAt + 16 i.  No register is written, so the
-// compiler, which would otherwise wait for all copies before any LDS read, need not know; whoever reads the tile waits by wait_loads.
+// Copies twice 16 bytes a lane from global memory straight into LDS: lane i's from `from` + offset to `to` + kAt + 16 i, then kAt + 1024 + 16 i.  No register is
+// written, so the compiler, which would otherwise wait for all copies before any LDS read, need not know; whoever reads the tile waits by wait_loads.
+// `from` comes out of vector instructions (readlane), and a vector memory instruction that reads a scalar register needs five wait states after
+// a vector instruction's write to it.  The compiler adds none before inline assembly, and may move `from` between two statements of it, so each statement
+// has its own: the addition to m0 and four of s_nop 3.  m0 itself needs one before the copy.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"  // m0 is the compiler's own register; it keeps nothing there from one instruction to the next
 template <int kAt>
-__device__ __forceinline__ void copy_to_lds(uint64_t from, uint32_t offset, uint32_t to) {
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to), "n"(kAt) : "memory", "m0", "scc");
+__device__ __forceinline__ void copy_to_lds(uint64_t from, uint32_t offset0, uint32_t offset1, uint32_t to) {
+    asm volatile(
+        "s_add_u32 m0, %3, %4\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %2\n\t"
+        "s_add_u32 m0, %3, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"v"(offset0),
+        "v"(offset1), "s"(from), "s"(to), "n"(kAt), "n"(kAt + 1024)
+        : "memory", "m0", "scc");
 }
 #pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
@@ -457,12 +464,10 @@ __device__ __forceinline__ void attend(const AttentionArgs& a, const Item& w, ui
             const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)addresses, (int)(first + i));
             const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(addresses >> 32), (int)(first + i));
             const uint64_t from = (uint64_t)hi << 32 | lo;
-            copy_to_lds<0>(from, offset[0], to + i * 16 * kHead * 2);
-            copy_to_lds<1024>(from, offset[1], to + i * 16 * kHead * 2);
-            if constexpr (kCopies >= 4) copy_to_lds<2048>(from, offset[2], to + i * 16 * kHead * 2), copy_to_lds<3072>(from, offset[3], to + i * 16 * kHead * 2);
-            if constexpr (kCopies >= 8)
-                copy_to_lds<4096>(from, offset[4], to + i * 16 * kHead * 2), copy_to_lds<5120>(from, offset[5], to + i * 16 * kHead * 2),
-                    copy_to_lds<6144>(from, offset[6], to + i * 16 * kHead * 2), copy_to_lds<7168>(from, offset[7], to + i * 16 * kHead * 2);
+            const uint32_t at = to + i * 16 * kHead * 2;
+            copy_to_lds<0>(from, offset[0], offset[1], at);
+            if constexpr (kCopies >= 4) copy_to_lds<2048>(from, offset[2], offset[3], at);
+            if constexpr (kCopies >= 8) copy_to_lds<4096>(from, offset[4], offset[5], at), copy_to_lds<6144>(from, offset[6], offset[7], at);
             static_assert(kCopies == 2 || kCopies == 4 || kCopies == 8, "");
         }
     };
