@@ -44,7 +44,10 @@ def _on(stream, call, *args):
 
 
 def lsm_rope_table(n_positions: int, rot_dim: int, theta: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
-    """float32 [n_positions, rot_dim]: cosines, then sines, of the rotation's angles."""
+    """float32 [n_positions, rot_dim]: cosines, then sines, of the rotation's angles.  device: the current GPU ("cuda", or its own number)."""
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"device must be the current GPU, is {device}")
     L = _load()
     if not hasattr(L.lsm_rope_table, "typed"):
         L.lsm_rope_table.argtypes = [C.c_void_p, C.c_uint64, C.c_uint32, C.c_double, C.c_void_p]
@@ -53,6 +56,8 @@ def lsm_rope_table(n_positions: int, rot_dim: int, theta: float = 10000.0, devic
         raise ValueError("n_positions must not be negative and rot_dim be above 0")
     if stream is not None:
         return _on(stream, lsm_rope_table, n_positions, rot_dim, theta, device)
+    if device.index not in (None, torch.cuda.current_device()):
+        raise ValueError(f"device must be the current GPU ({torch.cuda.current_device()}), is {device}")
     table = torch.empty((n_positions, rot_dim), dtype=torch.float32, device=device)
     rc = L.lsm_rope_table(table.data_ptr(), n_positions, rot_dim, theta, _stream_ptr(None))
     if rc != 0:
