@@ -65,8 +65,9 @@ struct AttentionArgs {
     uint32_t whole, tiles[2], splits[2], wide[2], combos[2], combos_part[2], least[2], items0;
     uint32_t joined;  // the parts are joined by another kernel
     float* part_out;  // [split of either stage][KV head][row][head_dim]
-    float2* part_ml;  // [split of either stage][KV head][row]: maximum in units of the exponent of two, sum
+    float2* part_ml;  // [split of either stage][KV head][row]: maximum in units of the exponent of two, sum; kNoPart = there is no part
 };
+constexpr float kNoPart = -1.f;  // no sum of weights
 
 // x / d for x < 2^31, given part_of(d): a division takes forty instructions, and a workgroup's first pass over its instructions is most of a short call.
 inline uint32_t part_of(uint32_t d) { return 0xFFFFFFFFu / d; }
@@ -765,8 +766,8 @@ __global__ void __launch_bounds__(kThreads, kHead == 256 ? 1 : 2) attention_kern
     const uint32_t units = units_of(w.len[0]) + units_of(w.len[1]), each = split_units(units, stage ? a.splits[1] : a.splits[0], stage ? a.least[1] : a.least[0]);
     w.unit0 = split * each, w.unit1 = w.unit0 + each < units ? w.unit0 + each : units;
     w.part = ((uint64_t)((stage ? a.splits[0] : 0) + split) * a.kv_heads + kv_head) * a.rows;
-    if (a.joined && w.unit0 >= units) {  // not one of the ranges that there are: its part is empty
-        if (threadIdx.x < tile_rows && w.row0 + threadIdx.x < w.row_end) a.part_ml[w.part + w.row0 + threadIdx.x] = make_float2(-__builtin_inff(), 0.f);
+    if (a.joined && w.unit0 >= units) {  // not one of the ranges that there are
+        if (threadIdx.x < tile_rows && w.row0 + threadIdx.x < w.row_end) a.part_ml[w.part + w.row0 + threadIdx.x] = make_float2(-__builtin_inff(), kNoPart);
         return;
     }
     if (wide) attend<kType, kHead, true>(a, w, kv_head, lds);
@@ -774,7 +775,7 @@ __global__ void __launch_bounds__(kThreads, kHead == 256 ? 1 : 2) attention_kern
 }
 
 // Joins a row's parts in the order of their numbers.  kHead / 4 lanes have a row; first each has the maxima and sums of some of its parts (at most 128 in
-// all), then four columns of all of them.
+// all), then four columns of all of them.  A part whose weight is 0 is added like any other: it may hold an infinity or NaN, which a seen value put there.
 template <int kType, int kHead>
 __global__ void __launch_bounds__(kThreads) join_kernel(const AttentionArgs a) {
     typedef typename Half<kType>::type T;
@@ -789,7 +790,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttentionArgs a) {
     float most = -__builtin_inff();
 #pragma unroll
     for (uint32_t i = 0; i < kMine; i++) {
-        ml[i] = make_float2(-__builtin_inff(), 0.f);
+        ml[i] = make_float2(-__builtin_inff(), kNoPart);
         if (i * kLanes + in_row < parts) ml[i] = a.part_ml[(i * kLanes + in_row) * all + at];
         most = fmaxf(most, ml[i].x);
     }
@@ -799,8 +800,9 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttentionArgs a) {
     float sum = 0.f;
 #pragma unroll
     for (uint32_t i = 0; i < kMine; i++) {
-        ml[i].x = ml[i].x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - base);
-        sum += ml[i].y * ml[i].x;
+        const bool none = ml[i].y == kNoPart;
+        ml[i].x = none ? kNoPart : __builtin_amdgcn_exp2f(ml[i].x - base);
+        if (!none) sum += ml[i].y * ml[i].x;
     }
 #pragma unroll
     for (uint32_t off = 1; off < kLanes; off <<= 1) sum += __shfl_xor(sum, (int)off, kWave);
@@ -816,9 +818,9 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const AttentionArgs a) {
             float by[4];
 #pragma unroll
             for (uint32_t u = 0; u < 4; u++) {
-                by[u] = j + u < left ? __shfl(ml[i].x, (int)(lane - in_row + j + u), kWave) : 0.f;
+                by[u] = j + u < left ? __shfl(ml[i].x, (int)(lane - in_row + j + u), kWave) : kNoPart;
                 v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (by[u] != 0.f) v[u] = *reinterpret_cast<const float4*>(from + (i * kLanes + j + u) * all * kHead);  // an empty part's are not written
+                if (by[u] != kNoPart) v[u] = *reinterpret_cast<const float4*>(from + (i * kLanes + j + u) * all * kHead);
             }
 #pragma unroll
             for (uint32_t u = 0; u < 4; u++) o.x += v[u].x * by[u], o.y += v[u].y * by[u], o.z += v[u].z * by[u], o.w += v[u].w * by[u];
