@@ -33,8 +33,11 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
 }
 bool given(PyObject* o) { return o != Py_None; }
 
-void check_device(const at::Tensor& t, const char* what, c10::DeviceIndex device) {
+void check_gpu(const at::Tensor& t, const char* what) {
     if (!t.is_cuda()) throw BadArgument(std::string(what) + " must be a GPU tensor");
+}
+void check_device(const at::Tensor& t, const char* what, c10::DeviceIndex device) {
+    check_gpu(t, what);
     if (t.get_device() != device) throw BadArgument(std::string(what) + " must be on the current device");
 }
 
@@ -121,6 +124,12 @@ lsm_rotation_t rotation(const at::Tensor& x, c10::DeviceIndex device, PyObject* 
 
 const void* weight_data(PyObject* o) { return given(o) ? THPVariable_Unpack(o).data_ptr() : nullptr; }
 
+// The current device, asked for once there is a GPU tensor: without a GPU this would be the first thing to fail.
+c10::DeviceIndex device_for(const at::Tensor& t, const char* what) {
+    check_gpu(t, what);
+    return c10::hip::current_device();
+}
+
 // A call's body: BadArgument and whatever torch throws become Python errors, an error code of the library its number.
 template <typename F>
 PyObject* call(Py_ssize_t n, Py_ssize_t want, F body) {
@@ -155,9 +164,10 @@ PyObject* none() { Py_RETURN_NONE; }
 PyObject* rotate_heads(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 10, [&]() -> PyObject* {
         if (!given(o[0]) && !given(o[1])) throw BadArgument("lsm_rotate_heads needs q or k");
-        const c10::DeviceIndex device = c10::hip::current_device();
-        const at::Tensor& x = given(o[0]) ? tensor(o[0], "q") : tensor(o[1], "k");
-        check_device(x, given(o[0]) ? "q" : "k", device);
+        const char* const first = given(o[0]) ? "q" : "k";
+        const at::Tensor& x = tensor(given(o[0]) ? o[0] : o[1], first);
+        const c10::DeviceIndex device = device_for(x, first);
+        check_device(x, first, device);
         const lsm_rotation_t how = rotation(x, device, o[2], o[3], o[4], o[5], o[6], o[7]);
         lsm_heads_t in[2] = {}, out[2] = {};
         at::Tensor result[2];
@@ -178,8 +188,8 @@ PyObject* rotate_heads(PyObject*, PyObject* const* o, Py_ssize_t n) {
 // k, v, positions, slots, k_pages, v_pages, table, k_weight, q, q_weight, q_out, eps, interleaved
 PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 13, [&]() -> PyObject* {
-        const c10::DeviceIndex device = c10::hip::current_device();
         const at::Tensor &k = tensor(o[0], "k"), &v = tensor(o[1], "v"), &k_pages = tensor(o[4], "k_pages"), &v_pages = tensor(o[5], "v_pages");
+        const c10::DeviceIndex device = device_for(k, "k");
         check_device(k, "k", device);
         const lsm_rotation_t how = rotation(k, device, o[2], o[6], o[9], o[7], o[11], o[12]);
         const at::ScalarType type = k.scalar_type();
@@ -207,9 +217,9 @@ PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
 // q, k_pages, v_pages, group_offsets, prefix_tables, prefix_lens, q_offsets, own_tables, own_lens, scale, with_lse, out, workspace
 PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 13, [&]() -> PyObject* {
-        const c10::DeviceIndex device = c10::hip::current_device();
         const at::Tensor &q = tensor(o[0], "q"), &k_pages = tensor(o[1], "k_pages"), &v_pages = tensor(o[2], "v_pages");
         const at::Tensor &prefix_tables = tensor(o[4], "prefix_tables"), &own_tables = tensor(o[7], "own_tables");
+        const c10::DeviceIndex device = device_for(q, "q");
         check_device(q, "q", device);
         const at::ScalarType type = q.scalar_type();
         if (type != at::kBFloat16 && type != at::kHalf) throw BadArgument(std::string("q must be bfloat16 or float16, is ") + c10::toString(type));

@@ -19,3 +19,31 @@ def test_rope_table_is_made_on_the_current_gpu_alone(monkeypatch, device):
     monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("memory was taken"))
     with pytest.raises(ValueError, match="device"):
         lsm.lsm_rope_table(8, 64, device=device)
+
+
+def calls(**change):
+    """The three calls on tensors of matching shapes, some of them exchanged."""
+    import paper_2511_16138_amd as lsm
+    t = dict(q=torch.zeros(2, 4, 64, dtype=torch.bfloat16), k=torch.zeros(2, 2, 64, dtype=torch.bfloat16), v=torch.zeros(2, 2, 64, dtype=torch.bfloat16),
+             pages=torch.zeros(3, 16, 2, 64, dtype=torch.bfloat16), w=torch.ones(64), positions=torch.zeros(2, dtype=torch.int32), slots=torch.zeros(2, dtype=torch.int64),
+             table=torch.zeros(8, 64), out=None)
+    t.update(change)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=getattr(t["v"], "device", "cpu"))  # noqa: E731
+    batch = lsm.PrefixBatch(ints([0, 2]), ints([[0]]), ints([16]), ints([0, 1, 2]), ints([[1], [2]]), ints([1, 1]))
+    return {
+        "rotate": lambda: lsm.lsm_rotate_heads(t["q"], t["k"], t["positions"], t["table"], q_weight=t["w"], q_out=t["out"]),
+        "append": lambda: lsm.lsm_kv_append(t["k"], t["v"], t["positions"], t["slots"], t["pages"], t["pages"], t["table"], k_weight=t["w"], q=t["q"], q_out=t["out"]),
+        "attend": lambda: lsm.lsm_prefix_attention(t["q"], t["pages"], t["pages"], batch, out=t["out"]),
+    }
+
+
+@pytest.mark.parametrize("name, what", [("rotate", "q"), ("append", "k"), ("attend", "q")])
+def test_host_tensors_raise_value_error_with_or_without_a_gpu(name, what):
+    with pytest.raises(ValueError, match=f"^{what} must be a GPU tensor"):
+        calls()[name]()
+
+
+@pytest.mark.parametrize("name", ["rotate", "append", "attend"])
+def test_what_is_no_tensor_raises_value_error_with_or_without_a_gpu(name):
+    with pytest.raises(ValueError, match="must be a tensor"):
+        calls(**({"pages": 5} if name == "attend" else {"k": 5, "q": 5}))[name]()
