@@ -9,6 +9,7 @@ Tensors are on the current GPU:
 
 Work goes to torch's current stream, or to `stream` (a torch stream or a HIP stream handle), which is then the current one while
 outputs and workspace are made.  Wrong shapes and types raise ValueError, errors of the library LsmError; nothing is launched then.
+There is no backward pass and no forward mode: an input or output that requires gradients (where torch's grad mode is on) or has a tangent raises ValueError.
 The marshalling is compiled (csrc/lsm_cache_torch.cpp); there is no fallback: a missing module raises at the first call.
 """
 from __future__ import annotations

@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -32,6 +33,18 @@ const at::Tensor& tensor(PyObject* o, const char* what) {
     return THPVariable_Unpack(o);
 }
 bool given(PyObject* o) { return o != Py_None; }
+
+// These calls have no backward pass and no forward mode: their outputs would be constants to either, and nothing would tell.
+void check_constants(PyObject* const* o, const char* const* names, Py_ssize_t n) {
+    const c10::AutogradState& state = c10::AutogradState::get_tls_state();
+    const bool backward = state.get_grad_mode(), forward = state.get_fw_grad_mode();
+    for (Py_ssize_t i = 0; i < n; i++) {
+        if (!given(o[i]) || !THPVariable_Check(o[i])) continue;
+        const at::Tensor& t = THPVariable_Unpack(o[i]);
+        if (backward && t.requires_grad()) throw BadArgument(std::string(names[i]) + " requires gradients, and there is no backward pass: detach() it, or call under torch.no_grad()");
+        if (forward && t._fw_grad(0).defined()) throw BadArgument(std::string(names[i]) + " has a tangent, and there is no forward mode: take its primal");
+    }
+}
 
 void check_gpu(const at::Tensor& t, const char* what) {
     if (!t.is_cuda()) throw BadArgument(std::string(what) + " must be a GPU tensor");
@@ -160,9 +173,10 @@ PyObject* pair(PyObject* a, PyObject* b) {  // takes both references
 }
 PyObject* none() { Py_RETURN_NONE; }
 
-// q, k, positions, table, q_weight, k_weight, eps, interleaved, q_out, k_out
+constexpr const char* kRotateHeads[] = {"q", "k", "positions", "table", "q_weight", "k_weight", "eps", "interleaved", "q_out", "k_out"};
 PyObject* rotate_heads(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 10, [&]() -> PyObject* {
+        check_constants(o, kRotateHeads, n);
         if (!given(o[0]) && !given(o[1])) throw BadArgument("lsm_rotate_heads needs q or k");
         const char* const first = given(o[0]) ? "q" : "k";
         const at::Tensor& x = tensor(given(o[0]) ? o[0] : o[1], first);
@@ -185,9 +199,10 @@ PyObject* rotate_heads(PyObject*, PyObject* const* o, Py_ssize_t n) {
     });
 }
 
-// k, v, positions, slots, k_pages, v_pages, table, k_weight, q, q_weight, q_out, eps, interleaved
+constexpr const char* kKvAppend[] = {"k", "v", "positions", "slots", "k_pages", "v_pages", "table", "k_weight", "q", "q_weight", "q_out", "eps", "interleaved"};
 PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 13, [&]() -> PyObject* {
+        check_constants(o, kKvAppend, n);
         const at::Tensor &k = tensor(o[0], "k"), &v = tensor(o[1], "v"), &k_pages = tensor(o[4], "k_pages"), &v_pages = tensor(o[5], "v_pages");
         const c10::DeviceIndex device = device_for(k, "k");
         check_device(k, "k", device);
@@ -214,9 +229,10 @@ PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
     });
 }
 
-// q, k_pages, v_pages, group_offsets, prefix_tables, prefix_lens, q_offsets, own_tables, own_lens, scale, with_lse, out, workspace
+constexpr const char* kPrefixAttention[] = {"q", "k_pages", "v_pages", "group_offsets", "prefix_tables", "prefix_lens", "q_offsets", "own_tables", "own_lens", "scale", "with_lse", "out", "workspace"};
 PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 13, [&]() -> PyObject* {
+        check_constants(o, kPrefixAttention, n);
         const at::Tensor &q = tensor(o[0], "q"), &k_pages = tensor(o[1], "k_pages"), &v_pages = tensor(o[2], "v_pages");
         const at::Tensor &prefix_tables = tensor(o[4], "prefix_tables"), &own_tables = tensor(o[7], "own_tables");
         const c10::DeviceIndex device = device_for(q, "q");

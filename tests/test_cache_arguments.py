@@ -47,3 +47,30 @@ def test_host_tensors_raise_value_error_with_or_without_a_gpu(name, what):
 def test_what_is_no_tensor_raises_value_error_with_or_without_a_gpu(name):
     with pytest.raises(ValueError, match="must be a tensor"):
         calls(**({"pages": 5} if name == "attend" else {"k": 5, "q": 5}))[name]()
+
+
+@pytest.mark.parametrize("name, which", [("rotate", "q"), ("rotate", "k"), ("rotate", "w"), ("rotate", "table"), ("rotate", "out"), ("append", "k"), ("append", "v"),
+                                         ("append", "q"), ("append", "w"), ("append", "pages"), ("append", "out"), ("attend", "q"), ("attend", "pages"), ("attend", "out")])
+@pytest.mark.parametrize("kind", ["gradients", "tangent"])
+def test_inputs_with_gradients_or_tangents_are_refused(name, which, kind):
+    """There is no backward pass and no forward mode: outputs would be without a word about it constants of either."""
+    from torch.autograd import forward_ad
+
+    def run(want):
+        shapes = dict(q=(2, 4, 64), k=(2, 2, 64), v=(2, 2, 64), pages=(3, 16, 2, 64), w=(64,), table=(8, 64), out=(2, 4, 64))
+        x = torch.zeros(shapes[which], dtype=torch.float32 if which in ("w", "table") else torch.bfloat16)
+        x = x.requires_grad_() if kind == "gradients" else forward_ad.make_dual(x, torch.ones_like(x))
+        # on the CPU: whatever has no gradients or tangents is refused for being no GPU tensor
+        with pytest.raises(ValueError) as e:
+            calls(**{which: x})[name]()
+        assert (kind in str(e.value)) == want, str(e.value)
+
+    if kind == "gradients":
+        run(True)
+        with torch.no_grad():
+            run(False)
+    else:
+        with forward_ad.dual_level():
+            run(True)
+            with forward_ad._set_fwd_grad_enabled(False):
+                run(False)
