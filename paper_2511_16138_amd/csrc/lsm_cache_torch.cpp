@@ -88,6 +88,11 @@ const I* ints(PyObject* o, const char* what, c10::DeviceIndex device, at::IntArr
     return static_cast<const I*>(t.data_ptr());
 }
 
+// A caller's tensor was written: whoever saved it for a gradient has to find out.  (Inference tensors count no writes.)
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 at::Tensor new_like(const at::Tensor& t) { return at::empty(t.sizes(), t.options().requires_grad(false).memory_format(at::MemoryFormat::Contiguous)); }
 
 double number(PyObject* o) {
@@ -195,6 +200,8 @@ PyObject* rotate_heads(PyObject*, PyObject* const* o, Py_ssize_t n) {
         }
         const int rc = lsm_rotate_heads(&how, given(o[0]) ? &in[0] : nullptr, weight_data(o[4]), &out[0], given(o[1]) ? &in[1] : nullptr, weight_data(o[5]), &out[1], stream_of(device));
         if (rc != LSM_OK) return PyLong_FromLong(rc);
+        for (int i = 0; i < 2; i++)
+            if (given(o[i]) && given(o[8 + i])) written(result[i]);
         return pair(given(o[0]) ? THPVariable_Wrap(result[0]) : none(), given(o[1]) ? THPVariable_Wrap(result[1]) : none());
     });
 }
@@ -225,6 +232,8 @@ PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
         const int rc = lsm_kv_append(&how, &hk, weight_data(o[7]), &hv, slots, &pk, &pv, (uint64_t)k_pages.size(0), (uint64_t)k_pages.size(1),
                                      given(o[8]) ? &hq : nullptr, weight_data(o[9]), &ho, stream_of(device));
         if (rc != LSM_OK) return PyLong_FromLong(rc);
+        written(k_pages), written(v_pages);
+        if (given(o[8]) && given(o[10])) written(result);
         return given(o[8]) ? THPVariable_Wrap(result) : none();
     });
 }
@@ -278,6 +287,8 @@ PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
         }
         const int rc = lsm_prefix_attention(&a, ws, bytes, stream_of(device));
         if (rc != LSM_OK) return PyLong_FromLong(rc);
+        if (given(o[11])) written(out);
+        if (given(o[12])) written(tensor(o[12], "workspace"));
         return with_lse ? pair(THPVariable_Wrap(out), THPVariable_Wrap(lse)) : THPVariable_Wrap(out);
     });
 }

@@ -37,6 +37,27 @@ def attend(lsm, t):
     return lsm.lsm_prefix_attention(t["q"], t["k_pages"], t["v_pages"], batch, out=t["out"], workspace=t["workspace"])
 
 
+def test_in_place_writes_are_counted(lsm):
+    """A graph that saved a tensor finds out that it was written since."""
+    t = tensors(out=torch.zeros(2, 4, 64, dtype=BF16, device="cuda"))
+    blocks = torch.zeros(3, 2, 16, 2, 64, dtype=BF16, device="cuda")
+    t["k_pages"], t["v_pages"] = blocks[:, 0], blocks[:, 1]
+    t["q_out"], t["k_out"] = t["q"], t["k"]
+    before = {n: t[n]._version for n in ("q", "k", "out")}, blocks._version
+    rotate(lsm, t)
+    assert t["q"]._version == before[0]["q"] + 1 and t["k"]._version == before[0]["k"] + 1
+    append(lsm, t)
+    assert t["q"]._version == before[0]["q"] + 2 and blocks._version > before[1]
+    attend(lsm, t)
+    assert t["out"]._version == before[0]["out"] + 1
+    assert all(t[n]._version == 0 for n in ("v", "positions", "slots", "table", "q_weight", "own_tables"))
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    saved = (t["out"] * w.to(BF16)).sum()  # saves `out` for the gradient of w
+    attend(lsm, t)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        saved.backward()
+
+
 def test_inference_tensors_are_taken(lsm):
     with torch.inference_mode():
         t = tensors(out=torch.zeros(2, 4, 64, dtype=BF16, device="cuda"))
