@@ -842,6 +842,8 @@ static bool aligned_rows(const void* data, int64_t s0, int64_t s1, int64_t s2) {
     return ((reinterpret_cast<uint64_t>(data) | (uint64_t)(s0 * 2) | (uint64_t)(s1 * 2) | (uint64_t)(s2 * 2)) & 15) == 0;
 }
 
+constexpr float kLog2E = 1.44269504088896341f;  // scores are scaled by this too: weights are powers of two
+
 static int check_attention(const lsm_attention_t* a) {
     if (a == nullptr) return LSM_ERR_NULL;
     if (a->dtype != LSM_BF16 && a->dtype != LSM_FP16) return LSM_ERR_BAD_ARG;
@@ -850,7 +852,7 @@ static int check_attention(const lsm_attention_t* a) {
     if (a->kv_heads == 0 || a->q.heads == 0 || a->q.heads != a->out.heads || a->q.heads % a->kv_heads != 0 || a->q.heads > 4096) return LSM_ERR_BAD_ARG;
     if (a->n_tokens >= 1u << 24 || a->n_tokens * a->q.heads >= 1ull << 31 || a->n_requests >= 1u << 24 || a->n_groups >= 1u << 24 || a->n_pages >= 1ull << 31) return LSM_ERR_BAD_ARG;
     if (a->prefix_width * a->page_tokens >= 1ull << 30 || a->own_width * a->page_tokens >= 1ull << 30 || a->prefix_width >= 1u << 30 || a->own_width >= 1u << 30) return LSM_ERR_BAD_ARG;
-    if (a->reserved != 0 || !(a->scale > 0.f) || a->scale > 3.0e38f) return LSM_ERR_BAD_ARG;
+    if (a->reserved != 0 || !(a->scale > 0.f) || !(a->scale * kLog2E < __builtin_inff())) return LSM_ERR_BAD_ARG;
     if (a->n_tokens == 0) return LSM_OK;
     if (a->n_requests == 0) return LSM_ERR_BAD_ARG;
     if (a->q.data == nullptr || a->out.data == nullptr || a->q_offsets == nullptr || a->own_lens == nullptr) return LSM_ERR_NULL;
@@ -970,7 +972,7 @@ extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, s
     p.n_tokens = (uint32_t)a->n_tokens, p.n_requests = (uint32_t)a->n_requests, p.n_groups = (uint32_t)a->n_groups, p.n_pages = (uint32_t)a->n_pages;
     p.page_shift = (uint32_t)__builtin_ctzll(a->page_tokens);
     p.prefix_width = a->n_groups ? a->prefix_width : 0, p.own_width = a->own_width;
-    p.scale = a->scale * 1.44269504088896341f;
+    p.scale = a->scale * kLog2E;
     p.part_out = static_cast<float*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + (size_t)(p.splits[0] + p.splits[1]) * a->n_tokens * a->q.heads * a->head_dim * 4);
     hipStream_t s = static_cast<hipStream_t>(stream);
