@@ -76,7 +76,7 @@ typedef struct {
 /*
  * lsm_rope_table -- table[p][i] = cos(p theta^(-2i / rot_dim)), table[p][rot_dim / 2 + i] = the sine, for p < n_positions
  * and i < rot_dim / 2; angles, cosines and sines in 64 bits (an angle of 10^5 held in 32 bits is off by 4e-3), rounded once.
- * Errors: LSM_ERR_NULL, LSM_ERR_BAD_ARG (rot_dim odd, 0 or > LSM_MAX_HEAD_DIM, theta not above 0), LSM_ERR_HIP.
+ * Errors: LSM_ERR_NULL, LSM_ERR_BAD_ARG (rot_dim odd, 0 or > LSM_MAX_HEAD_DIM, theta not above 0 or infinite), LSM_ERR_HIP.
  */
 int lsm_rope_table(float* table, uint64_t n_positions, uint32_t rot_dim, double theta, void* stream);
 

@@ -466,7 +466,7 @@ static int launch_rotate(RotateArgs& a, const lsm_rotation_t* how, hipStream_t s
 using namespace lsm;
 
 extern "C" int lsm_rope_table(float* table, uint64_t n_positions, uint32_t rot_dim, double theta, void* stream) {
-    if (rot_dim == 0 || rot_dim % 2 != 0 || rot_dim > LSM_MAX_HEAD_DIM || !(theta > 0.0) || n_positions >= 1ull << 31) return LSM_ERR_BAD_ARG;
+    if (rot_dim == 0 || rot_dim % 2 != 0 || rot_dim > LSM_MAX_HEAD_DIM || !(theta > 0.0) || !(theta < __builtin_inf()) || n_positions >= 1ull << 31) return LSM_ERR_BAD_ARG;
     if (n_positions == 0) return LSM_OK;
     if (table == nullptr) return LSM_ERR_NULL;
     if (reinterpret_cast<uint64_t>(table) & 3) return LSM_ERR_BAD_ARG;

@@ -19,3 +19,8 @@ def attend(lib, a):
 def test_a_scale_that_is_infinite_for_exponents_of_two_is_refused(lib, scale):
     """The kernels multiply scores by scale log2(e): beyond 3.4e38 / 1.4427 that is infinite, and a score of 0 becomes NaN."""
     assert attend(lib, attention(scale=scale)) == (0, BAD)
+
+
+def test_an_infinite_base_of_angles_is_refused(lib):
+    """Its logarithm times 0, the exponent of the first pair, is no number."""
+    assert lib.lsm_rope_table(AT, 8, 64, math.inf, None) == BAD
