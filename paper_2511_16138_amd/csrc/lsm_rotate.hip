@@ -391,6 +391,7 @@ static int check_rotation(const lsm_rotation_t* how) {
 }
 
 constexpr uint64_t kMostHeads = 1u << 16;
+constexpr uint64_t kMostBlocks = (1ull << 24) - 1;  // of 256 threads
 
 // One of the parts with an output of its own: queries, or keys of lsm_rotate_heads.
 static int set_heads(HeadsView& v, const lsm_rotation_t* how, const lsm_heads_t* in, const void* weight, const lsm_heads_t* out) {
@@ -452,12 +453,23 @@ static int launch_rotate(RotateArgs& a, const lsm_rotation_t* how, hipStream_t s
     const uint32_t each = (rounds + slices - 1) / slices;
     a.heads_per_slice = each * at_once;
     a.slices = (heads + a.heads_per_slice - 1) / a.heads_per_slice;
-    const uint64_t waves = a.n_tokens * a.slices;
-    const uint64_t blocks = (waves + 3) / 4;
-    if (waves >= 1ull << 31) return LSM_ERR_BAD_ARG;
-    if (how->dtype == LSM_BF16) launch_type<LSM_BF16>(a, lanes, (uint32_t)blocks, stream);
-    else if (how->dtype == LSM_FP16) launch_type<LSM_FP16>(a, lanes, (uint32_t)blocks, stream);
-    else launch_type<LSM_FP32>(a, lanes, (uint32_t)blocks, stream);
+    // A launch has fewer than 2^32 threads (one of more is cut without an error): more tokens than that, 64 threads each, take several.
+    const uint64_t all = a.n_tokens, most = kMostBlocks * 4 / a.slices;
+    for (uint64_t first = 0; first < all; first += most) {
+        a.n_tokens = all - first < most ? all - first : most;
+        const uint32_t blocks = (uint32_t)((a.n_tokens * a.slices + 3) / 4);
+        if (how->dtype == LSM_BF16) launch_type<LSM_BF16>(a, lanes, blocks, stream);
+        else if (how->dtype == LSM_FP16) launch_type<LSM_FP16>(a, lanes, blocks, stream);
+        else launch_type<LSM_FP32>(a, lanes, blocks, stream);
+        for (int p = 0; p < 3; p++) {
+            HeadsView& v = a.part[p];
+            const int64_t step = (int64_t)a.n_tokens * element_bytes(how->dtype);
+            v.in = static_cast<const char*>(v.in) + step * v.in_token;
+            if (p == 0 || a.slots == nullptr) v.out = static_cast<char*>(v.out) + step * v.out_token;  // keys and values go to pages otherwise
+        }
+        if (a.positions != nullptr) a.positions += a.n_tokens;
+        if (a.slots != nullptr) a.slots += a.n_tokens;
+    }
     return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
 }
 
