@@ -116,7 +116,8 @@ int lsm_kv_append(const lsm_rotation_t* how, const lsm_heads_t* k, const void* k
  * Rows behind a length, and pages that no length reaches, are never used, whatever they hold; keys and values that are not
  * finite reach the tokens that see them and no others.
  * Offsets that descend or leave their range give an unspecified, in-bounds result.
- * scale: above 0, and scale log2(e) finite.
+ * scale: above 0, and scale log2(e) finite.  n_tokens, n_requests and n_groups are below 2^24, n_tokens * q.heads below 2^31,
+ * widths times page_tokens below 2^30; a batch is one launch of fewer than 2^24 workgroups (about 1.8 million decodes of 8 KV heads).
  * dtype: LSM_BF16 or LSM_FP16; head_dim: 64, 128 or 256.  The weights of the softmax are rounded to dtype for the product
  * with the values, as the values are.  All rows 16-byte aligned: data 16-byte aligned, strides multiples of 8.
  * workspace: DEVICE, 256-byte aligned, lsm_prefix_attention_workspace_bytes(a) bytes; contents on entry are irrelevant.

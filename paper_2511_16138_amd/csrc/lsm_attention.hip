@@ -922,25 +922,34 @@ static void plan_attention(const lsm_attention_t* a, AttentionArgs& p) {
     p.joined = !(p.whole && p.splits[1] == 1);
 }
 
+// A launch has fewer than 2^32 threads; one of more is cut without an error.
+static uint64_t join_blocks(const lsm_attention_t* a) {
+    const uint64_t per_block = kWaves * kWave * 4 / a->head_dim;
+    return (a->n_tokens * a->q.heads + per_block - 1) / per_block;
+}
+static bool fits_launches(const lsm_attention_t* a, const AttentionArgs& p) {
+    constexpr uint64_t kMost = (1ull << 32) / kThreads - 1;
+    return ((uint64_t)p.tiles[0] * p.splits[0] + (uint64_t)p.tiles[1] * p.splits[1]) * p.kv_heads <= kMost && (!p.joined || join_blocks(a) <= kMost);
+}
+
 static size_t part_bytes(const lsm_attention_t* a, const AttentionArgs& p) {
     if (!p.joined) return 0;
     return (size_t)(p.splits[0] + p.splits[1]) * a->n_tokens * a->q.heads * (a->head_dim * 4 + 8);
 }
 
 template <int kType, int kHead>
-static void launch(const AttentionArgs& p, uint32_t blocks, hipStream_t stream) {
+static void launch(const AttentionArgs& p, uint32_t blocks, uint32_t joins, hipStream_t stream) {
     if (!p.whole) hipLaunchKernelGGL((attention_kernel<kType, kHead, kBoth>), dim3(blocks), dim3(kThreads), 0, stream, p);
     else if (p.wide[1]) hipLaunchKernelGGL((attention_kernel<kType, kHead, kWideAlone>), dim3(blocks), dim3(kThreads), 0, stream, p);
     else hipLaunchKernelGGL((attention_kernel<kType, kHead, kNarrowAlone>), dim3(blocks), dim3(kThreads), 0, stream, p);
     if (!p.joined) return;
-    const uint64_t all = (uint64_t)p.n_tokens * p.share * p.kv_heads, per_block = kWaves * (kWave / (kHead / 4));
-    hipLaunchKernelGGL((join_kernel<kType, kHead>), dim3((uint32_t)((all + per_block - 1) / per_block)), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((join_kernel<kType, kHead>), dim3(joins), dim3(kThreads), 0, stream, p);
 }
 template <int kType>
-static void launch_type(const AttentionArgs& p, uint32_t head, uint32_t blocks, hipStream_t stream) {
-    if (head == 64) launch<kType, 64>(p, blocks, stream);
-    else if (head == 128) launch<kType, 128>(p, blocks, stream);
-    else launch<kType, 256>(p, blocks, stream);
+static void launch_type(const AttentionArgs& p, uint32_t head, uint32_t blocks, uint32_t joins, hipStream_t stream) {
+    if (head == 64) launch<kType, 64>(p, blocks, joins, stream);
+    else if (head == 128) launch<kType, 128>(p, blocks, joins, stream);
+    else launch<kType, 256>(p, blocks, joins, stream);
 }
 
 }  // namespace lsm
@@ -951,7 +960,7 @@ extern "C" size_t lsm_prefix_attention_workspace_bytes(const lsm_attention_t* a)
     if (check_attention(a) != LSM_OK || a->n_tokens == 0) return 0;
     AttentionArgs p = {};
     plan_attention(a, p);
-    return part_bytes(a, p);
+    return fits_launches(a, p) ? part_bytes(a, p) : 0;
 }
 
 extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, size_t workspace_bytes, void* stream) {
@@ -959,10 +968,10 @@ extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, s
     if (rc != LSM_OK || a->n_tokens == 0) return rc;
     AttentionArgs p = {};
     plan_attention(a, p);
+    if (!fits_launches(a, p)) return LSM_ERR_BAD_ARG;
     const size_t need = part_bytes(a, p);
     if (need != 0 && (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uint64_t>(workspace) & 255) != 0)) return LSM_ERR_WORKSPACE;
-    if (((uint64_t)p.tiles[0] * p.splits[0] + (uint64_t)p.tiles[1] * p.splits[1]) * p.kv_heads >= 1ull << 30) return LSM_ERR_BAD_ARG;
-    const uint64_t blocks = (uint64_t)p.items0 + (uint64_t)p.tiles[1] * p.combos[1];
+    const uint32_t blocks = p.items0 + p.tiles[1] * p.combos[1], joins = p.joined ? (uint32_t)join_blocks(a) : 0;
     p.q = a->q.data, p.out = a->out.data, p.lse = a->lse, p.k = a->k_pages.data, p.v = a->v_pages.data;
     p.q_token = a->q.token_stride, p.q_head = a->q.head_stride, p.out_token = a->out.token_stride, p.out_head = a->out.head_stride;
     p.k_page = (uint32_t)a->k_pages.page_stride * 2, p.k_token = (uint32_t)a->k_pages.token_stride * 2, p.k_head = (uint64_t)a->k_pages.head_stride * 2;
@@ -976,7 +985,7 @@ extern "C" int lsm_prefix_attention(const lsm_attention_t* a, void* workspace, s
     p.part_out = static_cast<float*>(workspace);
     p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + (size_t)(p.splits[0] + p.splits[1]) * a->n_tokens * a->q.heads * a->head_dim * 4);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (a->dtype == LSM_BF16) launch_type<LSM_BF16>(p, a->head_dim, (uint32_t)blocks, s);
-    else launch_type<LSM_FP16>(p, a->head_dim, (uint32_t)blocks, s);
+    if (a->dtype == LSM_BF16) launch_type<LSM_BF16>(p, a->head_dim, blocks, joins, s);
+    else launch_type<LSM_FP16>(p, a->head_dim, blocks, joins, s);
     return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
 }

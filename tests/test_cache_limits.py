@@ -24,3 +24,20 @@ def test_a_scale_that_is_infinite_for_exponents_of_two_is_refused(lib, scale):
 def test_an_infinite_base_of_angles_is_refused(lib):
     """Its logarithm times 0, the exponent of the first pair, is no number."""
     assert lib.lsm_rope_table(AT, 8, 64, math.inf, None) == BAD
+
+
+@pytest.mark.parametrize("change", [
+    # HIP takes launches of fewer than 2^32 threads, 256 a workgroup here
+    dict(n_tokens=3 << 20, n_requests=3 << 20, n_groups=0, own_width=1),                                      # 3M decodes, 8 KV heads: 25M workgroups
+    dict(n_tokens=3 << 20, n_requests=3 << 20, n_groups=1, own_width=1, prefix_width=1 << 20),                # behind a prefix
+    dict(n_tokens=1 << 22, n_requests=1 << 20, n_groups=1, own_width=4, prefix_width=1 << 12, kv_heads=1, q=test_cache_host.Heads(AT, 8192, 128, 64),
+         out=test_cache_host.Heads(AT, 8192, 128, 64)),                                                       # 5M workgroups, but 32M join their parts
+])
+def test_batches_of_more_workgroups_than_a_launch_takes_are_refused(lib, change):
+    assert attend(lib, attention(**change)) == (0, BAD)
+
+
+def test_the_largest_batches_have_a_workspace(lib):
+    """A million decodes of 8 KV heads behind a prefix: 10M workgroups, and 4M that join their parts."""
+    a = attention(n_tokens=(1 << 20), n_requests=(1 << 20), n_groups=1, own_width=1, prefix_width=1 << 20)
+    assert lib.lsm_prefix_attention_workspace_bytes(C.byref(a)) > 0
