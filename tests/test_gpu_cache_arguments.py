@@ -137,3 +137,32 @@ def test_errors_of_the_library_are_raised(lsm):
     with pytest.raises(ValueError):
         lsm.lsm_rope_table(8, 64, device="cpu")
     assert lsm.lsm_rope_table(8, 64, device=f"cuda:{torch.cuda.current_device()}").shape == (8, 64)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_work_goes_to_the_stream_that_is_named(lsm, handle):
+    """`stream`, a torch stream or its handle: inputs that it is still writing are waited for, and the current stream is as it was."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    t = tensors(table=lsm.lsm_rope_table(8, 64))
+    rand = lambda x: torch.randn(x.shape, generator=gen, device="cuda").to(x.dtype)  # noqa: E731
+    new = {n: rand(t[n]) for n in ("q", "k", "v", "k_pages", "v_pages", "q_weight", "k_weight")}
+    plain = {**t, **{n: x.clone() for n, x in new.items()}}
+    want = [*rotate(lsm, plain), append(lsm, plain), attend(lsm, plain), plain["k_pages"], plain["v_pages"]]
+    torch.cuda.synchronize()
+    side, current = torch.cuda.Stream(), torch.cuda.current_stream()
+    on = dict(stream=side.cuda_stream if handle else side)
+    big = torch.randn(2048, 2048, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            big = big @ big * 1e-3
+        for n, x in new.items():
+            t[n].copy_(x)  # behind the products
+    batch = lsm.PrefixBatch(*(t[n] for n in ("group_offsets", "prefix_tables", "prefix_lens", "q_offsets", "own_tables", "own_lens")))
+    got = [*lsm.lsm_rotate_heads(t["q"], t["k"], t["positions"], t["table"], q_weight=t["q_weight"], k_weight=t["k_weight"], **on),
+           lsm.lsm_kv_append(t["k"], t["v"], t["positions"], t["slots"], t["k_pages"], t["v_pages"], t["table"], k_weight=t["k_weight"], q=t["q"], q_weight=t["q_weight"], **on),
+           lsm.lsm_prefix_attention(t["q"], t["k_pages"], t["v_pages"], batch, **on), t["k_pages"], t["v_pages"]]
+    table = lsm.lsm_rope_table(8, 64, **on)
+    assert torch.cuda.current_stream() == current
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(table, t["table"])

@@ -185,3 +185,19 @@ def test_two_stages_keep_what_is_not_finite_from_tokens_before_it(lsm, i):
     finite = torch.isfinite(out.cpu()).all(-1).all(-1)
     ends = [sum(q_lens[:r + 1]) - 1 for r in range(len(q_lens))]
     assert (~finite).nonzero().flatten().tolist() == ends
+
+
+@pytest.mark.parametrize("way, groups, q_lens, hq, hkv, joined", [
+    ("narrow alone", [1] * 130, [1] * 130, 4, 1, False), ("narrow alone", [1, 0, 2] * 50, [1 + i % 3 for i in range(150)], 8, 2, False),
+    ("wide alone", [1] * 70, [20 + i % 9 for i in range(70)], 4, 1, False), ("narrow alone", [0] * 64 + [2] + [0] * 70 + [1], [1, 2, 1], 4, 1, False)])
+def test_one_pass_over_more_than_64_groups(lsm, way, groups, q_lens, hq, hkv, joined):
+    """Every request finds its group, however many there are and however many of them are empty."""
+    gen = torch.Generator().manual_seed(31)
+    n = len(q_lens)
+    prefix = [(7 * i) % 90 for i in range(len(groups))]
+    q, blocks, parts = make_batch(gen, groups, prefix, q_lens, [m + i % 30 for i, m in enumerate(q_lens)], hq, hkv, 64, 16, BF16)
+    assert int(parts[0][-1]) == n
+    out, lse = attend(lsm, q, blocks, parts, way, joined)
+    want, want_lse, bound, lse_bound = ref.attention(q, blocks[:, 0], blocks[:, 1], *parts)
+    ref.assert_within(out, want, bound, "out")
+    ref.assert_within(lse, want_lse, lse_bound, "lse")
