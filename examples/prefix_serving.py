@@ -75,7 +75,7 @@ class Server:
         hit_len, hits = self.index.probe(keys, counts)
         blocks = (hits[..., 0] & 0xFFFFFFFF).tolist()  # value pointer = block number
         for r, n, found in zip(requests, hit_len.tolist(), blocks):
-            n = min(n, (len(r.tokens) - 1) // BLOCK)   # at least one token has to be run for its output
+            n = max(0, min(n, (len(r.tokens) - 1) // BLOCK))  # at least one token has to be run for its output
             r.blocks, r.cached, r.found = found[:n], n * BLOCK, n * BLOCK
 
     def enter(self, requests: List[Request]) -> None:
@@ -98,6 +98,9 @@ class Server:
     # -- one pass over new tokens ---------------------------------------------------------------------------------
     def plan(self, requests: List[Request]):
         """The batch in an order in which requests that share blocks are neighbours: (order, PrefixBatch, positions, slots, new tokens)."""
+        wanted = sum(max(0, -(-len(r.tokens) // BLOCK) - len(r.blocks)) for r in requests)
+        if any(not 0 < len(r.tokens) <= self.table.shape[0] for r in requests) or wanted > len(self.free):
+            raise ValueError(f"requests must have 1 to {self.table.shape[0]} tokens and fit the pool: {wanted} blocks wanted, {len(self.free)} free")
         for r in requests:
             while len(r.blocks) * BLOCK < len(r.tokens):
                 r.blocks.append(self.free.pop())

@@ -59,3 +59,15 @@ def test_served_batches_agree_with_a_plain_forward_pass(dtype, head_dim):
     third = [Request(list(second[0].tokens) + draw(4)), Request(list(second[1].tokens))]
     check(s.prefill(third), third)
     assert third[0].found == 96 and third[1].found == 32  # the prompt's own complete blocks
+
+
+def test_requests_that_cannot_be_served_are_refused_before_anything_is_taken():
+    """Without tokens, of more than there are angles for, or of more blocks than there are free: such batches gave logits of other tokens or NaN."""
+    from prefix_serving import Request, Server
+    s = Server(layers=1, heads=2, kv_heads=1, head_dim=64, width=32, vocab=20, blocks=5, max_tokens=96)
+    for tokens in ([], [1] * 97, [1] * 81):
+        requests = [Request([1, 2, 3]), Request(tokens)]
+        with pytest.raises(ValueError):
+            s.prefill(requests)
+        assert len(s.free) == 5 and not any(r.blocks for r in requests)
+    assert bool(torch.isfinite(s.prefill([Request([1] * 60), Request([2])])).all())
