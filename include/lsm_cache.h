@@ -92,8 +92,9 @@ int lsm_rotate_heads(const lsm_rotation_t* how, const lsm_heads_t* q, const void
 /*
  * lsm_kv_append -- keys (normed and rotated) and values (as they are) of token t go to slot slots[t] of the cache: page
  * slots[t] / page_tokens, row slots[t] % page_tokens.  A slot below 0 or not below n_pages * page_tokens writes nothing
- * (padding, tokens that are cached already).  Two tokens with one slot: either may win, per 16 bytes.  The queries of the
- * same tokens, skipped or not, are normed and rotated in the same launch if q is given, as lsm_rotate_heads does.
+ * (padding, tokens that are cached already).  Two tokens with one slot: either may win, for every 16 bytes, or
+ * every element where rows are not 16-byte aligned.  The queries of the same tokens, skipped or not, are normed and rotated
+ * in the same launch if q is given, as lsm_rotate_heads does.  Tokens beyond 2^26 take several launches, there and here.
  * slots: DEVICE, n_tokens int64.  k, v: the same number of heads.  page_tokens: any number above 0.
  * Errors: LSM_ERR_NULL, LSM_ERR_BAD_ARG, LSM_ERR_HIP.
  */
@@ -117,9 +118,12 @@ int lsm_kv_append(const lsm_rotation_t* how, const lsm_heads_t* k, const void* k
  * finite reach the tokens that see them and no others.
  * Offsets that descend or leave their range give an unspecified, in-bounds result.
  * scale: above 0, and scale log2(e) finite.  n_tokens, n_requests and n_groups are below 2^24, n_tokens * q.heads below 2^31,
- * widths times page_tokens below 2^30; a batch is one launch of fewer than 2^24 workgroups (about 1.8 million decodes of 8 KV heads).
+ * widths times page_tokens below 2^30; a batch is one launch of fewer than 2^24 workgroups (about 1.8 million decodes of
+ * 8 KV heads).
  * dtype: LSM_BF16 or LSM_FP16; head_dim: 64, 128 or 256.  The weights of the softmax are rounded to dtype for the product
- * with the values, as the values are.  All rows 16-byte aligned: data 16-byte aligned, strides multiples of 8.
+ * with the values, as the values are; in LSM_FP16 those under 2^-14 lose bits as subnormals, so that n keys far below the
+ * largest score are off by up to n 2^-25 of its weight.
+ * All rows 16-byte aligned: data 16-byte aligned, strides multiples of 8.
  * workspace: DEVICE, 256-byte aligned, lsm_prefix_attention_workspace_bytes(a) bytes; contents on entry are irrelevant.
  * Results are the same bits from call to call.  Errors: LSM_ERR_NULL, LSM_ERR_BAD_ARG, LSM_ERR_WORKSPACE, LSM_ERR_HIP.
  */

@@ -9,8 +9,12 @@
 // Measured, with the floor of bytes at a copy's 4.94 TB/s or of operations at a library product's 1.38 PFLOP/s:
 //   96 decodes of up to 8,000 keys, 4 KV heads of 128     180 us, 4.9 TB/s     (178: memory)
 //   64 decodes behind 8 prefixes of 512 - 1,536, 8 heads    30 us, 3.2 TB/s     (19: memory, then the way in and the join)
-//   256 decodes behind 8,192 and 16,384, 2 heads           127 us, 0.53 PFLOP/s (65: the matrix cores on the prefixes, then memory on the own pages)
-//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096        967 us, 0.98 PFLOP/s (686: matrix cores 52 % busy at 1.7 GHz, the softmax's vector instructions as long)
+//   256 decodes behind 8,192 and 16,384, 2 heads           126 us, 0.53 PFLOP/s (65: the matrix cores on the prefixes, then memory on the own pages)
+//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096        920 - 950 us, 1.01 PFLOP/s (686: matrix cores 51 % busy at 1.7 GHz, the softmax's vector instructions as long)
+// The weights of the softmax are rounded to 16 bits for the second product, which the matrix cores take no other operands for at this rate; with that the
+// error against 64 bits is 1.4 times that of a computation in 32 bits rounded once at the end (2.3e-3 and 1.7e-3 in bf16, 2.8e-4 and 2.1e-4 in fp16).
+// In fp16, weights under 2^-14 lose bits as subnormals and those under 2^-25 are 0 in the product, though not in the sum: many keys that far below the
+// maximum count for less (or more) than they should, by at most their number times 2^-25.
 #include <hip/hip_runtime.h>
 
 #include "lsm_cache.h"
@@ -256,7 +260,8 @@ struct Team {
         return most == -__builtin_inff() ? 0.f : -most * scale;  // a row that has seen nothing: all weights 0
     }
 
-    // Weights 2 i and 2 i + 1 of a lane, rounded to nearest as the values are; the sum is of the weights before that.
+    // Weights 2 i and 2 i + 1 of a lane, rounded to nearest as the values are, since the matrix cores take operands of one type (the head of this file has the
+    // error); the sum is of the weights before that.
     __device__ __forceinline__ void weight_pair(const Scores& s, Weights& p, uint32_t i, float scale, float base, float& more) {
         const uint32_t b = i / 8, j = i % 8 * 2;
         const f32x2 e = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], scale, base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j + 1], scale, base))};
@@ -718,7 +723,8 @@ __global__ void __launch_bounds__(kThreads, kHead == 256 ? 1 : 2) attention_kern
     // The first stage's items come first: one launch has both run side by side at the seam, and items bound by the matrix cores are not slowed down
     // by others that keep memory busy, as they are where the two take turns.
     const uint32_t stage = kStages != kBoth || blockIdx.x >= a.items0 ? 1 : 0, item = blockIdx.x - (kStages == kBoth && stage ? a.items0 : 0);
-    // The rows of a tile change last: workgroups that read the same keys are a multiple of the heads and ranges apart, and with eight of these on one die.
+    // The rows of a tile change last: workgroups that read the same keys are a multiple of the heads times ranges apart, and so on one die where that
+    // is a multiple of eight (8 KV heads); where it is not (2 KV heads, 5 ranges), several dies read them (256 decodes: 465 MB fetched, 319 due).
     const uint32_t combos = stage ? a.combos[1] : a.combos[0], tile = divide(item, combos, stage ? a.combos_part[1] : a.combos_part[0]), combo = item - tile * combos;
     if (tile >= (stage ? a.tiles[1] : a.tiles[0])) return;
     uint32_t split = 0, kv_head = combo;
