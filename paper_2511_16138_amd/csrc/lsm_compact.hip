@@ -2493,14 +2493,19 @@ extern "C" int lsm_range_scan(const lsm_ranges_t* ranges, const lsm_tree_t* tree
         rt.n[j] = r.n;
     }
     ModeArgs ma = {};
-    ma.lo_keys = ranges->lo_keys;
-    ma.hi_keys = ranges->hi_keys;
-    ma.counts = out->counts;
     ma.max_entries = ranges->max_entries;
     Workspace ws = {};
-    hipLaunchKernelGGL((merge_kernel<0, kModeRange>), dim3(ranges->n_ranges), dim3(kMergeThreads), 0, static_cast<hipStream_t>(stream_v), rt, ws,
-                       (uint64_t)ranges->n_ranges, (uint32_t)LSM_BOTTOMMOST, out->entries, (uint64_t*)nullptr, (const uint64_t*)nullptr, 0u,
-                       (uint4*)nullptr, 1u, ma);
+    // A launch has fewer than 2^32 threads (one of more is cut without an error): more ranges than that take several.
+    constexpr uint64_t kMostRanges = (1ull << 32) / kMergeThreads - 1;
+    for (uint64_t first = 0; first < ranges->n_ranges; first += kMostRanges) {
+        const uint64_t n = ranges->n_ranges - first < kMostRanges ? ranges->n_ranges - first : kMostRanges;
+        ma.lo_keys = ranges->lo_keys + first * LSM_KEY_BYTES;
+        ma.hi_keys = ranges->hi_keys + first * LSM_KEY_BYTES;
+        ma.counts = out->counts + first;
+        hipLaunchKernelGGL((merge_kernel<0, kModeRange>), dim3((uint32_t)n), dim3(kMergeThreads), 0, static_cast<hipStream_t>(stream_v), rt, ws, n,
+                           (uint32_t)LSM_BOTTOMMOST, out->entries + first * ranges->max_entries, (uint64_t*)nullptr, (const uint64_t*)nullptr, 0u,
+                           (uint4*)nullptr, 1u, ma);
+    }
     return hipGetLastError() == hipSuccess ? LSM_OK : LSM_ERR_HIP;
 }
 
