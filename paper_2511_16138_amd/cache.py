@@ -1,10 +1,12 @@
-"""The paged-cache calls of liblsm_index.so (include/lsm_cache.h; same names as the C entry points) on torch tensors.
+"""The paged-cache calls of liblsm_index.so (include/lsm_cache.h, include/lsm_pages.h; same names as the C entry points) on torch tensors.
 
 Tensors are on the current GPU:
   q, k, v          [n_tokens, heads, head_dim], any strides with contiguous elements of a head; bfloat16, float16 (or float32,
                    not for attention)
   k_pages, v_pages [n_pages, page_tokens, kv_heads, head_dim], any strides likewise: a layer's slice of blocks that hold all
                    layers' keys and values is fine
+                   in 8 bits: float8_e4m3fn, with
+  k_scales, v_scales float8_e8m0fnu [n_pages, page_tokens / 16, kv_heads], any strides: a value is code * scale, one scale for 16 tokens of a head
   positions, page tables, lengths, offsets   int32, contiguous;  slots   int64, contiguous
 
 Work goes to torch's current stream, or to `stream` (a torch stream or a HIP stream handle), which is then the current one while
@@ -16,7 +18,7 @@ from __future__ import annotations
 
 import ctypes as C
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import List, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -110,15 +112,57 @@ class PrefixBatch:
 
 
 def lsm_prefix_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, batch: PrefixBatch, *, scale: Optional[float] = None,
-                         with_lse: bool = False, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
-    """Attention of a batch whose requests share prefixes: out [n_tokens, heads, head_dim], or (out, lse [n_tokens, heads])."""
-    call = (_calls or _module()).prefix_attention
+                         with_lse: bool = False, k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                         out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of a batch whose requests share prefixes: out [n_tokens, heads, head_dim], or (out, lse [n_tokens, heads]).
+
+    k_scales, v_scales: the pages are in 8 bits.  window: a token sees the last `window` tokens of its sequence (prefix, then own), itself among them, and
+    the first `sinks`; 0: all of them.  (lsm_window_attention of the C library, where any of these is given.)"""
+    more = k_scales is not None or v_scales is not None or window != 0 or sinks != 0
+    call = (_calls or _module()).window_attention if more else (_calls or _module()).prefix_attention
     b = batch
-    if stream is None:
-        r = call(q, k_pages, v_pages, b.group_offsets, b.prefix_tables, b.prefix_lens, b.q_offsets, b.own_tables, b.own_lens, scale, with_lse, out, workspace)
-    else:
-        r = _on(stream, call, q, k_pages, v_pages, b.group_offsets, b.prefix_tables, b.prefix_lens, b.q_offsets, b.own_tables, b.own_lens, scale, with_lse,
-                out, workspace)
+    args = (q, k_pages, v_pages, b.group_offsets, b.prefix_tables, b.prefix_lens, b.q_offsets, b.own_tables, b.own_lens, scale, with_lse, out, workspace)
+    if more:
+        args += (k_scales, v_scales, window, sinks)
+    r = call(*args) if stream is None else _on(stream, call, *args)
     if type(r) is int:
-        raise LsmError(r, "lsm_prefix_attention")
+        raise LsmError(r, "lsm_window_attention" if more else "lsm_prefix_attention")
     return r
+
+
+def lsm_kv_append8(k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor], batch: PrefixBatch, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                   k_scales: torch.Tensor, v_scales: torch.Tensor, table: Optional[torch.Tensor], *, k_weight: Optional[torch.Tensor] = None,
+                   q: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                   eps: float = 1e-6, interleaved: bool = False, stream=None) -> Optional[torch.Tensor]:
+    """Keys (normed, rotated) and values of the batch's new tokens into pages of 8 bits, where lsm_prefix_attention looks for them; returns q normed and
+    rotated if it is given.  Of the batch, q_offsets, own_tables and own_lens count."""
+    call = (_calls or _module()).kv_append8
+    b = batch
+    args = (k, v, positions, b.q_offsets, b.own_tables, b.own_lens, k_pages, v_pages, k_scales, v_scales, table, k_weight, q, q_weight, q_out, eps, interleaved)
+    r = call(*args) if stream is None else _on(stream, call, *args)
+    if type(r) is int:
+        raise LsmError(r, "lsm_kv_append8")
+    return r
+
+
+def lsm_copy_pages(pages: Union[torch.Tensor, Sequence[torch.Tensor]], sources: torch.Tensor, targets: torch.Tensor, *, stream=None) -> None:
+    """Page targets[i] becomes a copy of page sources[i] in every tensor [n_pages, ...] of any type whose pages are single stretches of memory."""
+    call = (_calls or _module()).copy_pages
+    r = call(pages, sources, targets) if stream is None else _on(stream, call, pages, sources, targets)
+    if type(r) is int:
+        raise LsmError(r, "lsm_copy_pages")
+
+
+def lsm_compact_pages(pages: Union[torch.Tensor, Sequence[torch.Tensor]], tables: Union[torch.Tensor, Sequence[torch.Tensor]],
+                      lens: Union[torch.Tensor, Sequence[torch.Tensor]], page_tokens: int, *, n_pages: Optional[int] = None,
+                      stream=None) -> Tuple[List[torch.Tensor], torch.Tensor, torch.Tensor]:
+    """Moves the pages that the tables hold together: (new tables, moved [n_pages], n_live [1]).  Entry j of a row of a table [rows, width] holds a page if
+    j * page_tokens < lens[row]; moved is a page's new number, -1 for a free one; pages from n_live on are free afterwards.  pages: as for lsm_copy_pages, or [] with
+    n_pages given, for the plan alone."""
+    call = (_calls or _module()).compact_pages
+    args = (pages, tables, lens, page_tokens, n_pages)
+    r = call(*args) if stream is None else _on(stream, call, *args)
+    if type(r) is int:
+        raise LsmError(r, "lsm_compact_pages")
+    new_tables, (moved, n_live) = r
+    return new_tables, moved, n_live

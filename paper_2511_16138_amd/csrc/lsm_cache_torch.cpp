@@ -11,10 +11,13 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
 #include "lsm_cache.h"
+#include "lsm_pages.h"
 
 namespace {
 
@@ -74,6 +77,16 @@ lsm_pages_t pages(const at::Tensor& t, const char* what, c10::DeviceIndex device
     return lsm_pages_t{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
 }
 
+lsm_scales_t scales(PyObject* o, const char* what, c10::DeviceIndex device, const at::Tensor& pages) {
+    const at::Tensor& t = tensor(o, what);
+    check_device(t, what, device);
+    if (t.scalar_type() != at::kFloat8_e8m0fnu) throw BadArgument(std::string(what) + " must be Float8_e8m0fnu, is " + c10::toString(t.scalar_type()));
+    const int64_t want[3] = {pages.size(0), pages.size(1) / LSM_SCALE_TOKENS, pages.size(2)};
+    if (pages.size(1) % LSM_SCALE_TOKENS != 0 || t.sizes() != at::IntArrayRef(want, 3))
+        throw BadArgument(std::string(what) + " must be [n_pages, page_tokens / 16, kv_heads] for pages of " + shape_text(pages) + ", is " + shape_text(t));
+    return lsm_scales_t{static_cast<uint8_t*>(t.data_ptr()), t.stride(0), t.stride(1), t.stride(2)};
+}
+
 template <typename I>
 const I* ints(PyObject* o, const char* what, c10::DeviceIndex device, at::IntArrayRef shape) {
     const at::Tensor& t = tensor(o, what);
@@ -99,6 +112,12 @@ double number(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw BadArgument("");
     return v;
+}
+uint64_t whole(PyObject* o, const char* what) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw BadArgument("");
+    if (v < 0) throw BadArgument(std::string(what) + " must not be negative");
+    return (uint64_t)v;
 }
 bool truth(PyObject* o) {
     const int v = PyObject_IsTrue(o);
@@ -238,9 +257,12 @@ PyObject* kv_append(PyObject*, PyObject* const* o, Py_ssize_t n) {
     });
 }
 
-constexpr const char* kPrefixAttention[] = {"q", "k_pages", "v_pages", "group_offsets", "prefix_tables", "prefix_lens", "q_offsets", "own_tables", "own_lens", "scale", "with_lse", "out", "workspace"};
+constexpr const char* kPrefixAttention[] = {"q", "k_pages", "v_pages", "group_offsets", "prefix_tables", "prefix_lens", "q_offsets", "own_tables", "own_lens", "scale", "with_lse", "out", "workspace",
+                                            "k_scales", "v_scales", "window", "sinks"};
+// kMore: with the four arguments of lsm_window_attention.
+template <bool kMore>
 PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
-    return call(n, 13, [&]() -> PyObject* {
+    return call(n, kMore ? 17 : 13, [&]() -> PyObject* {
         check_constants(o, kPrefixAttention, n);
         const at::Tensor &q = tensor(o[0], "q"), &k_pages = tensor(o[1], "k_pages"), &v_pages = tensor(o[2], "v_pages");
         const at::Tensor &prefix_tables = tensor(o[4], "prefix_tables"), &own_tables = tensor(o[7], "own_tables");
@@ -261,7 +283,9 @@ PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
             lse = at::empty({tokens, q.size(1)}, q.options().dtype(at::kFloat).requires_grad(false));
             a.lse = static_cast<float*>(lse.data_ptr());
         }
-        a.k_pages = pages(k_pages, "k_pages", device, k_pages, type), a.v_pages = pages(v_pages, "v_pages", device, k_pages, type);
+        const bool in_8_bits = kMore && (given(o[13]) || given(o[14]) || k_pages.scalar_type() == at::kFloat8_e4m3fn);
+        const at::ScalarType held = in_8_bits ? at::kFloat8_e4m3fn : type;
+        a.k_pages = pages(k_pages, "k_pages", device, k_pages, held), a.v_pages = pages(v_pages, "v_pages", device, k_pages, held);
         a.group_offsets = ints<int32_t>(o[3], "group_offsets", device, {groups + 1});
         a.prefix_tables = ints<int32_t>(o[4], "prefix_tables", device, {groups, prefix_tables.size(1)});
         a.prefix_lens = ints<int32_t>(o[5], "prefix_lens", device, {groups});
@@ -273,19 +297,28 @@ PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
         a.n_pages = (uint64_t)k_pages.size(0), a.page_tokens = (uint64_t)k_pages.size(1), a.kv_heads = (uint64_t)k_pages.size(2);
         a.head_dim = (uint32_t)q.size(2), a.dtype = dtype_code(type);
         a.scale = given(o[9]) ? (float)number(o[9]) : (float)(1.0 / sqrt((double)q.size(2)));
+        lsm_window_attention_t w = {};
+        if constexpr (kMore) {
+            w.base = a, w.window = whole(o[15], "window"), w.sinks = whole(o[16], "sinks");
+            if (w.sinks != 0 && w.window == 0) throw BadArgument("sinks need a window");
+            if (in_8_bits) {
+                if (!given(o[13]) || !given(o[14])) throw BadArgument("pages of 8 bits need k_scales and v_scales");
+                w.k_scales = scales(o[13], "k_scales", device, k_pages), w.v_scales = scales(o[14], "v_scales", device, k_pages);
+            }
+        }
         at::Tensor workspace;
         void* ws = nullptr;
         size_t bytes = 0;
         if (given(o[12])) {
-            const at::Tensor& w = tensor(o[12], "workspace");
-            check_device(w, "workspace", device);
-            if (!w.is_contiguous()) throw BadArgument("workspace must be contiguous");
-            ws = w.data_ptr(), bytes = w.nbytes();
-        } else if ((bytes = lsm_prefix_attention_workspace_bytes(&a)) != 0) {
+            const at::Tensor& space = tensor(o[12], "workspace");
+            check_device(space, "workspace", device);
+            if (!space.is_contiguous()) throw BadArgument("workspace must be contiguous");
+            ws = space.data_ptr(), bytes = space.nbytes();
+        } else if ((bytes = kMore ? lsm_window_attention_workspace_bytes(&w) : lsm_prefix_attention_workspace_bytes(&a)) != 0) {
             workspace = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte).requires_grad(false));
             ws = workspace.data_ptr();
         }
-        const int rc = lsm_prefix_attention(&a, ws, bytes, stream_of(device));
+        const int rc = kMore ? lsm_window_attention(&w, ws, bytes, stream_of(device)) : lsm_prefix_attention(&a, ws, bytes, stream_of(device));
         if (rc != LSM_OK) return PyLong_FromLong(rc);
         if (given(o[11])) written(out);
         if (given(o[12])) written(tensor(o[12], "workspace"));
@@ -293,10 +326,153 @@ PyObject* prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
     });
 }
 
+constexpr const char* kKvAppend8[] = {"k", "v", "positions", "q_offsets", "own_tables", "own_lens", "k_pages", "v_pages", "k_scales", "v_scales", "table", "k_weight", "q", "q_weight", "q_out", "eps", "interleaved"};
+PyObject* kv_append8(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    return call(n, 17, [&]() -> PyObject* {
+        check_constants(o, kKvAppend8, n);
+        const at::Tensor &k = tensor(o[0], "k"), &v = tensor(o[1], "v"), &k_pages = tensor(o[6], "k_pages"), &v_pages = tensor(o[7], "v_pages"), &own_tables = tensor(o[4], "own_tables");
+        const c10::DeviceIndex device = device_for(k, "k");
+        check_device(k, "k", device);
+        const lsm_rotation_t how = rotation(k, device, o[2], o[10], o[13], o[11], o[15], o[16]);
+        const at::ScalarType type = k.scalar_type();
+        const int64_t tokens = k.size(0), head_dim = k.size(2);
+        const lsm_heads_t hk = heads(k, "k", device, tokens, head_dim, type), hv = heads(v, "v", device, tokens, head_dim, type);
+        const lsm_pages_t pk = pages(k_pages, "k_pages", device, k_pages, at::kFloat8_e4m3fn), pv = pages(v_pages, "v_pages", device, k_pages, at::kFloat8_e4m3fn);
+        if (k_pages.size(2) != k.size(1) || k_pages.size(3) != head_dim || v.size(1) != k.size(1))
+            throw BadArgument("k_pages must be [n_pages, page_tokens, " + std::to_string(k.size(1)) + ", " + std::to_string(head_dim) + "] and v have as many heads as k; they are " + shape_text(k_pages) + " and " + shape_text(v));
+        const lsm_scales_t sk = scales(o[8], "k_scales", device, k_pages), sv = scales(o[9], "v_scales", device, k_pages);
+        if (own_tables.dim() != 2) throw BadArgument("own_tables must be [n_requests, own_width]");
+        const int64_t requests = own_tables.size(0);
+        lsm_new_tokens_t to = {};
+        to.q_offsets = ints<int32_t>(o[3], "q_offsets", device, {requests + 1});
+        to.own_tables = ints<int32_t>(o[4], "own_tables", device, {requests, own_tables.size(1)});
+        to.own_lens = ints<int32_t>(o[5], "own_lens", device, {requests});
+        to.n_requests = (uint64_t)requests, to.own_width = (uint64_t)own_tables.size(1), to.n_pages = (uint64_t)k_pages.size(0), to.page_tokens = (uint64_t)k_pages.size(1);
+        lsm_heads_t hq = {}, ho = {};
+        at::Tensor result;
+        if (given(o[12])) {
+            const at::Tensor& q = tensor(o[12], "q");
+            hq = heads(q, "q", device, tokens, head_dim, type);
+            result = given(o[14]) ? tensor(o[14], "q_out") : new_like(q);
+            ho = heads(result, "q_out", device, tokens, head_dim, type);
+        }
+        const int rc = lsm_kv_append8(&how, &hk, weight_data(o[11]), &hv, &to, &pk, &sk, &pv, &sv, given(o[12]) ? &hq : nullptr, weight_data(o[13]), &ho, stream_of(device));
+        if (rc != LSM_OK) return PyLong_FromLong(rc);
+        written(k_pages), written(v_pages), written(tensor(o[8], "k_scales")), written(tensor(o[9], "v_scales"));
+        if (given(o[12]) && given(o[14])) written(result);
+        return given(o[12]) ? THPVariable_Wrap(result) : none();
+    });
+}
+
+// The items of a list or tuple (a tensor alone is one item).
+std::vector<PyObject*> items(PyObject* o, const char* what) {
+    if (THPVariable_Check(o)) return {o};
+    if (!PyList_Check(o) && !PyTuple_Check(o)) throw BadArgument(std::string(what) + " must be a tensor, or a list or tuple of tensors");
+    PyObject** const first = PySequence_Fast_ITEMS(o);
+    return std::vector<PyObject*>(first, first + PySequence_Fast_GET_SIZE(o));
+}
+
+// Buffers of pages: the first dimension counts them, and a page is one stretch of memory.
+std::vector<lsm_page_part_t> page_parts(const std::vector<PyObject*>& list, c10::DeviceIndex device, int64_t n_pages) {
+    std::vector<lsm_page_part_t> parts;
+    for (PyObject* o : list) {
+        const at::Tensor& t = tensor(o, "pages");
+        const char* const name = "pages";
+        check_constants(&o, &name, 1);
+        check_device(t, "pages", device);
+        if (t.dim() < 1 || t.size(0) != n_pages) throw BadArgument("all buffers must have as many pages as the first one, " + std::to_string(n_pages) + "; one is " + shape_text(t));
+        std::vector<std::pair<int64_t, int64_t>> dims;  // stride, size
+        int64_t held = 1;
+        for (int64_t i = 1; i < t.dim(); i++) {
+            held *= t.size(i);
+            if (t.size(i) != 1) dims.push_back({t.stride(i), t.size(i)});
+        }
+        std::sort(dims.begin(), dims.end());
+        int64_t next = 1;
+        bool dense = true;
+        for (const auto& d : dims) dense = dense && d.first == next, next *= d.second;
+        if (held != 0 && !dense) throw BadArgument("a page must be one stretch of memory; one of the buffers has pages of " + shape_text(t) + " with gaps or overlaps");
+        if (held != 0 && n_pages > 1 && t.stride(0) < held) throw BadArgument("pages must not overlap");
+        parts.push_back(lsm_page_part_t{t.data_ptr(), t.stride(0) * t.element_size(), (uint64_t)(held * t.element_size())});
+    }
+    return parts;
+}
+
+constexpr const char* kCopyPages[] = {"sources", "targets"};
+PyObject* copy_pages(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    return call(n, 3, [&]() -> PyObject* {
+        check_constants(o + 1, kCopyPages, 2);
+        const std::vector<PyObject*> list = items(o[0], "pages");
+        const at::Tensor &sources = tensor(o[1], "sources"), &targets = tensor(o[2], "targets");
+        const c10::DeviceIndex device = device_for(sources, "sources");
+        check_device(sources, "sources", device);
+        if (sources.dim() != 1) throw BadArgument("sources must be int32 [n], is " + shape_text(sources));
+        const int32_t *from = ints<int32_t>(o[1], "sources", device, {sources.size(0)}), *to = ints<int32_t>(o[2], "targets", device, {sources.size(0)});
+        (void)targets;
+        if (list.empty()) return none();
+        const at::Tensor& first = tensor(list[0], "pages");
+        if (first.dim() < 1) throw BadArgument("pages must be [n_pages, ...]");
+        const std::vector<lsm_page_part_t> parts = page_parts(list, device, first.size(0));
+        const int rc = lsm_copy_pages(parts.data(), parts.size(), (uint64_t)first.size(0), from, to, (uint64_t)sources.size(0), stream_of(device));
+        if (rc != LSM_OK) return PyLong_FromLong(rc);
+        for (PyObject* p : list) written(THPVariable_Unpack(p));
+        return none();
+    });
+}
+
+// (pages, tables, lens, page_tokens, n_pages): the new tables, moved, n_live.
+PyObject* compact_pages(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    return call(n, 5, [&]() -> PyObject* {
+        const std::vector<PyObject*> list = items(o[0], "pages"), tables = items(o[1], "tables"), lens = items(o[2], "lens");
+        if (tables.size() != lens.size() || tables.empty() || tables.size() > LSM_MAX_PAGE_TABLES) throw BadArgument("there must be 1 to 16 tables, and lens for each");
+        const at::Tensor& lead = tensor(tables[0], "a table");
+        const c10::DeviceIndex device = device_for(lead, "a table");
+        int64_t n_pages;
+        if (!list.empty()) {
+            const at::Tensor& first = tensor(list[0], "pages");
+            if (first.dim() < 1) throw BadArgument("pages must be [n_pages, ...]");
+            n_pages = first.size(0);
+            if (given(o[4]) && whole(o[4], "n_pages") != (uint64_t)n_pages) throw BadArgument("n_pages is not what the buffers have, " + std::to_string(n_pages));
+        } else {
+            if (!given(o[4])) throw BadArgument("without buffers n_pages must be given");
+            n_pages = (int64_t)whole(o[4], "n_pages");
+            if (n_pages >= 1ll << 30) throw BadArgument("n_pages must be below 2^30");
+        }
+        const std::vector<lsm_page_part_t> parts = page_parts(list, device, n_pages);
+        std::vector<lsm_page_table_t> in;
+        std::vector<at::Tensor> out;
+        for (size_t i = 0; i < tables.size(); i++) {
+            const at::Tensor& t = tensor(tables[i], "a table");
+            if (t.dim() != 2) throw BadArgument("a table must be int32 [rows, width], is " + shape_text(t));
+            check_device(t, "a table", device);
+            const int32_t *held = ints<int32_t>(tables[i], "a table", device, {t.size(0), t.size(1)}), *lengths = ints<int32_t>(lens[i], "lens of a table", device, {t.size(0)});
+            out.push_back(new_like(t));
+            in.push_back(lsm_page_table_t{held, lengths, static_cast<int32_t*>(out.back().data_ptr()), (uint64_t)t.size(0), (uint64_t)t.size(1)});
+        }
+        const auto options = lead.options().requires_grad(false);
+        at::Tensor moved = at::empty({n_pages}, options), n_live = at::empty({1}, options);
+        const size_t bytes = lsm_compact_pages_workspace_bytes((uint64_t)n_pages);
+        at::Tensor workspace = at::empty({(int64_t)bytes}, options.dtype(at::kByte));
+        const int rc = lsm_compact_pages(parts.data(), parts.size(), (uint64_t)n_pages, whole(o[3], "page_tokens"), in.data(), in.size(), static_cast<int32_t*>(moved.data_ptr()),
+                                         static_cast<int32_t*>(n_live.data_ptr()), workspace.data_ptr(), bytes, stream_of(device));
+        if (rc != LSM_OK) return PyLong_FromLong(rc);
+        for (PyObject* p : list) written(THPVariable_Unpack(p));
+        PyObject* made = PyList_New((Py_ssize_t)out.size());
+        if (!made) return nullptr;
+        for (size_t i = 0; i < out.size(); i++) PyList_SET_ITEM(made, (Py_ssize_t)i, THPVariable_Wrap(out[i]));
+        PyObject* rest = pair(THPVariable_Wrap(moved), THPVariable_Wrap(n_live));
+        return pair(made, rest);
+    });
+}
+
 PyMethodDef kMethods[] = {
     {"rotate_heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotate_heads)), METH_FASTCALL, nullptr},
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append)), METH_FASTCALL, nullptr},
-    {"prefix_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prefix_attention)), METH_FASTCALL, nullptr},
+    {"prefix_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prefix_attention<false>)), METH_FASTCALL, nullptr},
+    {"window_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(prefix_attention<true>)), METH_FASTCALL, nullptr},
+    {"kv_append8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append8)), METH_FASTCALL, nullptr},
+    {"copy_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(copy_pages)), METH_FASTCALL, nullptr},
+    {"compact_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(compact_pages)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_cache", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
