@@ -11,9 +11,14 @@ that maps the key of a block (a digest of all tokens up to its end) to the block
   4. enters the new complete blocks into the index (LsmDriver.flush_unsorted), where later batches find them;
   5. decodes: one token per request and step, over the same pages.
 
+The pool may be held in 8 bits (in_8_bits: half the bytes, so twice the blocks; lsm_kv_append8 and scales in place of lsm_kv_append), and tokens may see a
+window of the last ones and the first few alone (window, sinks).  A request may go on in several ways (fork: whole blocks are shared, the one under way is
+copied by lsm_copy_pages), and blocks that neither the requests at hand nor the index hold any more are taken back by compact (lsm_compact_pages), which
+leaves the free ones in one stretch.
+
 The model is a stack of attention layers with random weights; nothing is learned or loaded.
 
-  python examples/prefix_serving.py            (on an MI355X)
+  python examples/prefix_serving.py [--in-8-bits] [--window]            (on an MI355X)
 """
 from __future__ import annotations
 
@@ -44,7 +49,8 @@ class Request:
 
 
 class Server:
-    def __init__(self, layers=4, heads=32, kv_heads=2, head_dim=128, width=1024, vocab=1000, blocks=4096, max_tokens=4096, dtype=torch.bfloat16, seed=0):
+    def __init__(self, layers=4, heads=32, kv_heads=2, head_dim=128, width=1024, vocab=1000, blocks=4096, max_tokens=4096, dtype=torch.bfloat16, seed=0,
+                 in_8_bits=False, window=0, sinks=0):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         rand = lambda *shape: torch.randn(shape, generator=gen, device="cuda")  # noqa: E731
         self.layers, self.heads, self.kv_heads, self.head_dim = layers, heads, kv_heads, head_dim
@@ -53,10 +59,14 @@ class Server:
         self.out = [(rand(heads * head_dim, width) / (heads * head_dim) ** 0.5).to(dtype) for _ in range(layers)]
         self.q_norm, self.k_norm = ([(1 + 0.1 * rand(head_dim)).to(dtype) for _ in range(layers)] for _ in range(2))
         self.table = lsm.lsm_rope_table(max_tokens, head_dim)
-        self.pool = torch.zeros((blocks, layers, 2, BLOCK, kv_heads, head_dim), dtype=dtype, device="cuda")
+        self.window, self.sinks, self.scales = window, sinks, None
+        self.pool = torch.zeros((blocks, layers, 2, BLOCK, kv_heads, head_dim), dtype=torch.float8_e4m3fn if in_8_bits else dtype, device="cuda")
+        if in_8_bits:
+            self.scales = torch.zeros((blocks, layers, 2, 1, kv_heads), dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
         self.free = list(range(blocks))
         self.index = lsm.LsmDriver(buffer_entries=1024, bloom_bits=16)
         self.seqno = 0
+        self.held = {}  # what the index has: the four words of a block's key -> its number
 
     # -- index ----------------------------------------------------------------------------------------------------
     @staticmethod
@@ -87,13 +97,52 @@ class Server:
                 rows.append((i, b, r.blocks[b]))
         if rows:
             i, b, block = torch.tensor(rows, device="cuda").T
-            entries = torch.zeros((len(rows), 8), dtype=torch.int64, device="cuda")
-            entries[:, :4] = keys[i, b]
-            entries[:, 4] = self.seqno + torch.arange(1, len(rows) + 1, device="cuda")
-            entries[:, 6], entries[:, 7] = block, self.pool[0].numel() * self.pool.element_size()
-            for part in entries.split(1024):
-                self.index.flush_unsorted(part.contiguous())
-            self.seqno += len(rows)
+            self.put(keys[i, b], block)
+
+    def put(self, keys: torch.Tensor, blocks: torch.Tensor) -> None:
+        """Enters blocks under their keys; a key that the index has already leads to its new block from now on."""
+        entries = torch.zeros((keys.shape[0], 8), dtype=torch.int64, device="cuda")
+        entries[:, :4] = keys
+        entries[:, 4] = self.seqno + torch.arange(1, keys.shape[0] + 1, device="cuda")
+        entries[:, 6], entries[:, 7] = blocks, self.pool[0].numel() * self.pool.element_size()
+        for part in entries.split(1024):
+            self.index.flush_unsorted(part.contiguous())
+        self.seqno += keys.shape[0]
+        self.held.update(zip(map(tuple, keys.tolist()), blocks.tolist()))
+
+    # -- blocks -----------------------------------------------------------------------------------------------------
+    def buffers(self):
+        return [self.pool] if self.scales is None else [self.pool, self.scales]
+
+    def fork(self, request: Request, n: int) -> List[Request]:
+        """n requests that go on from this one, which goes on itself: they share its whole blocks; the one under way is copied."""
+        under_way = len(request.tokens) % BLOCK != 0 and request.cached > len(request.tokens) // BLOCK * BLOCK
+        if request.cached != len(request.tokens) or under_way and n > len(self.free):
+            raise ValueError(f"a request that goes on has to have been run, and {n} blocks be free ({len(self.free)} are)")
+        made = [Request(list(request.tokens), list(request.blocks), request.cached, request.found) for _ in range(n)]
+        if under_way and n > 0:
+            own = [self.free.pop() for _ in range(n)]
+            for r, block in zip(made, own):
+                r.blocks[-1] = block
+            lsm.lsm_copy_pages(self.buffers(), torch.full((n,), request.blocks[-1], dtype=torch.int32, device="cuda"), torch.tensor(own, dtype=torch.int32, device="cuda"))
+        return made
+
+    def compact(self, requests: List[Request]) -> int:
+        """Takes back every block that neither these requests nor the index hold: held ones move together, requests and index go along.  How many are held."""
+        cached = list(self.held.items())
+        rows = [r.blocks for r in requests] + [[block for _, block in cached]]
+        wide = max(1, max(len(r) for r in rows))
+        table = torch.tensor([r + [-1] * (wide - len(r)) for r in rows], dtype=torch.int32, device="cuda")
+        lens = torch.tensor([len(r) * BLOCK for r in rows], dtype=torch.int32, device="cuda")
+        (table,), _, n_live = lsm.lsm_compact_pages(self.buffers(), [table], [lens], BLOCK)
+        new, n_live = table.tolist(), int(n_live)
+        for r, row in zip(requests, new):
+            r.blocks = row[:len(r.blocks)]
+        moved = [(key, block) for (key, old), block in zip(cached, new[-1]) if block != old]
+        if moved:
+            self.put(torch.tensor([k for k, _ in moved], device="cuda"), torch.tensor([b for _, b in moved], device="cuda"))
+        self.free = list(range(n_live, self.pool.shape[0]))
+        return n_live
 
     # -- one pass over new tokens ---------------------------------------------------------------------------------
     def plan(self, requests: List[Request]):
@@ -146,9 +195,14 @@ class Server:
             normed = (x * torch.rsqrt((x * x).mean(-1, keepdim=True) + 1e-6)).to(self.embedding.dtype)
             fused = (normed @ self.qkv[l]).view(-1, h + 2 * kv, self.head_dim)
             k_pages, v_pages = self.pool[:, l, 0], self.pool[:, l, 1]
-            q = lsm.lsm_kv_append(fused[:, h:h + kv], fused[:, h + kv:], positions, slots, k_pages, v_pages, self.table, k_weight=self.k_norm[l],
-                                  q=fused[:, :h], q_weight=self.q_norm[l])
-            o = lsm.lsm_prefix_attention(q, k_pages, v_pages, batch)
+            queries = dict(k_weight=self.k_norm[l], q=fused[:, :h], q_weight=self.q_norm[l])
+            scales = {}
+            if self.scales is None:
+                q = lsm.lsm_kv_append(fused[:, h:h + kv], fused[:, h + kv:], positions, slots, k_pages, v_pages, self.table, **queries)
+            else:
+                scales = dict(k_scales=self.scales[:, l, 0], v_scales=self.scales[:, l, 1])
+                q = lsm.lsm_kv_append8(fused[:, h:h + kv], fused[:, h + kv:], positions, batch, k_pages, v_pages, table=self.table, **scales, **queries)
+            o = lsm.lsm_prefix_attention(q, k_pages, v_pages, batch, window=self.window, sinks=self.sinks, **scales)
             x = x + (o.view(o.shape[0], -1) @ self.out[l]).float()
         last = x[batch.q_offsets[1:].long() - 1]
         for r in requests:
@@ -170,7 +224,7 @@ class Server:
 
 
 def main() -> None:
-    server = Server()
+    server = Server(in_8_bits="--in-8-bits" in sys.argv, window=512 if "--window" in sys.argv else 0, sinks=4 if "--window" in sys.argv else 0)
     gen = torch.Generator().manual_seed(1)
     draw = lambda n: torch.randint(0, 1000, (n,), generator=gen).tolist()  # noqa: E731
     prompts = [draw(512), draw(1024)]
@@ -185,6 +239,10 @@ def main() -> None:
         for _ in range(8):
             logits = server.decode(requests, logits.argmax(-1).tolist())
         print("  next tokens", logits.argmax(-1)[:8].tolist())
+        ways = [requests[0]] + server.fork(requests[0], 3)
+        logits = server.decode(ways, [1, 2, 3, 4])
+        print("  four ways to go on", logits.argmax(-1).tolist())
+    print(f"blocks held when all have ended: {server.compact([])}, free: {len(server.free)}")
 
 
 if __name__ == "__main__":

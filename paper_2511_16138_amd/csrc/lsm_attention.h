@@ -532,15 +532,14 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
         uint4 word[kMyBlocks][kLoads8 ? kLoads8 : 1];
         uint32_t scale[kMyBlocks];
     };
-    uint32_t k_from8[kLoads8], v_from8[kLoads8], k_to8[kLoads8], v_to8[kLoads8];
-#pragma unroll
-    for (uint32_t j = 0; j < kLoads8 && A::kIn8; j++) {
-        const uint32_t r = j * kRows8 + lane / kWords8, word = lane % kWords8;
-        k_from8[j] = r * a.k_token + word * 16, v_from8[j] = r * a.v_token + word * 16;
-        k_to8[j] = r * kHead * 2 + X::key_word(r, 2 * word) * 16, v_to8[j] = r * kHead * 2 + X::value_word(r, 2 * word) * 16;
-    }
-    auto fetch = [&](uint32_t t, uint64_t addresses, uint32_t scales, const uint32_t (&offset)[kLoads8], Raw& raw) {
-        const uint32_t first = first_lane(t) + (kWide ? wave : 0);
+    // What a lane's loads and stores go by is computed each time: kept in registers it would be spilled.
+    auto lane_again = [&]() {
+        uint32_t l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    auto fetch = [&](uint32_t t, uint64_t addresses, uint32_t scales, uint32_t token_stride, Raw& raw) {
+        const uint32_t first = first_lane(t) + (kWide ? wave : 0), l = lane_again(), offset = l / kWords8 * token_stride + l % kWords8 * 16;
 #pragma unroll
         for (uint32_t i = 0; i < kMyBlocks; i++) {
             const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)addresses, (int)(first + i));
@@ -548,11 +547,12 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
             raw.scale[i] = (uint32_t)__builtin_amdgcn_readlane((int)scales, (int)(first + i));
             const char* from = reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
 #pragma unroll
-            for (uint32_t j = 0; j < kLoads8; j++) raw.word[i][j] = *reinterpret_cast<const uint4*>(from + offset[j]);
+            for (uint32_t j = 0; j < kLoads8; j++) raw.word[i][j] = *reinterpret_cast<const uint4*>(from + j * kRows8 * token_stride + offset);
         }
     };
     // present: which of the tile's rows there are; zeros in place of the others
-    auto put = [&](const Raw& raw, const uint32_t (&offset)[kLoads8], char* to, uint64_t present) {
+    auto put = [&](const Raw& raw, bool keys, uint32_t to, uint64_t present) {
+        const uint32_t l = lane_again(), word = l % kWords8;
         if (kWide) to += wave * 16 * kHead * 2;
 #pragma unroll
         for (uint32_t i = 0; i < kMyBlocks; i++) {
@@ -560,11 +560,12 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
 #pragma unroll
             for (uint32_t j = 0; j < kLoads8; j++) {
                 const uint4 v = raw.word[i][j];
+                const uint32_t r = j * kRows8 + l / kWords8;  // of the block; tiles begin with whole blocks, so LDS words are permuted by this number
                 x8 lo = Half<kType>::decode8(v.x, v.y, scale), hi = Half<kType>::decode8(v.z, v.w, scale);
-                if (present != kAllKeys && !((present >> ((kWide ? wave : i) * 16 + j * kRows8 + lane / kWords8)) & 1)) lo = x8{}, hi = x8{};  // the scale may be NaN, too
-                char* at = to + i * 16 * kHead * 2 + offset[j];
-                *reinterpret_cast<x8*>(at) = lo;
-                *reinterpret_cast<x8*>(lds + ((uint32_t)(at - lds) ^ 16)) = hi;
+                if (present != kAllKeys && !((present >> ((kWide ? wave : i) * 16 + r)) & 1)) lo = x8{}, hi = x8{};  // the scale may be NaN, too
+                const uint32_t at = to + i * 16 * kHead * 2 + r * kHead * 2 + (keys ? X::key_word(r, 2 * word) : X::value_word(r, 2 * word)) * 16;
+                *reinterpret_cast<x8*>(lds + at) = lo;
+                *reinterpret_cast<x8*>(lds + (at ^ 16)) = hi;
             }
         }
     };
@@ -648,22 +649,22 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
     const uint32_t copies = lds_address(buffers);
     if (t < tile_end) find_pages(t);
     if constexpr (A::kIn8 && kWide) {
-        // As below, but what is asked for lands in registers and is put into LDS at the end of the iteration: values of the next tile, keys of the one after.
+        // Buffers as below.  What is asked for lands in registers, and is put into LDS where few others are in use: the keys of two tiles ahead at the top of an
+        // iteration, the next tile's values between scores and sums.  (Both at the end spill registers: 8 prompts 1,289 us.)
         if (t < tile_end) {
-            Raw k, v;
-            fetch(t, k_at, k_scale, k_from8, k);
-            fetch(t, v_at, v_scale, v_from8, v);
-            uint64_t present = keys_there(t), present_next = 0;
-            put(k, k_to8, buffers, kAllKeys);
+            Raw raw;
+            fetch(t, k_at, k_scale, a.k_token, raw);
+            uint64_t present = keys_there(t), present_next = t + 1 < tile_end ? keys_there(t + 1) : 0;
+            put(raw, true, 0, kAllKeys);
+            fetch(t, v_at, v_scale, a.v_token, raw);
+            put(raw, false, 2 * X::kBytes, present);
             if (t + 1 < tile_end) {
-                if (first_lane(t + 1) >= kWave) find_pages(t + 1);
-                fetch(t + 1, k_at, k_scale, k_from8, k);
-                present_next = keys_there(t + 1);
+                fetch(t + 1, k_at, k_scale, a.k_token, raw);
+                put(raw, true, X::kBytes, kAllKeys);
+                if (t + 2 < tile_end) fetch(t + 2, k_at, k_scale, a.k_token, raw);
             }
-            put(v, v_to8, buffers + 2 * X::kBytes, present);
             wait_lds();
             __builtin_amdgcn_s_barrier();
-            if (t + 1 < tile_end) put(k, k_to8, buffers + X::kBytes, kAllKeys);
             typename X::Scores s, next;
             typename X::Weights p;
             x.score(buffers, s);
@@ -675,24 +676,24 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
                 char* values = buffers + 2 * X::kBytes + buffer;
                 wait_lds();
                 __builtin_amdgcn_s_barrier();  // these values and the next keys are there, and everybody is done with these keys and the values before
-                const bool more = t + 1 < tile_end, after = t + 2 < tile_end;
+                const bool more = t + 1 < tile_end;
                 uint64_t present_after = 0;
-                if (more) {
-                    fetch(t + 1, v_at, v_scale, v_from8, v);
-                    if (after) {
-                        if (first_lane(t + 2) >= kWave) find_pages(t + 2);
-                        fetch(t + 2, k_at, k_scale, k_from8, k);
-                        present_after = keys_there(t + 2);
-                    }
-                }
+                if (t + 2 < tile_end) put(raw, true, buffer, kAllKeys);
+                if (more) fetch(t + 1, v_at, v_scale, a.v_token, raw);
                 const float base = x.rebase(top, a.scale);
                 keep_not_finite(t, values);
                 x.weights_and_score(s, p, a.scale, base, next_keys, next);
-                if (more) scores_masked(t + 1, present_next, next);
+                if (more) {
+                    scores_masked(t + 1, present_next, next);
+                    put(raw, false, 2 * X::kBytes + (buffer ^ X::kBytes), present_next);
+                    if (t + 2 < tile_end) {
+                        if (first_lane(t + 3) >= kWave) find_pages(t + 2);
+                        present_after = keys_there(t + 2);
+                        if (t + 3 < tile_end) fetch(t + 3, k_at, k_scale, a.k_token, raw);
+                    }
+                }
                 top = x.template weigh<true>(values, p, next);
                 if (!more) break;
-                put(v, v_to8, buffers + 2 * X::kBytes + (buffer ^ X::kBytes), present_next);
-                if (after) put(k, k_to8, buffers + buffer, kAllKeys);
                 for (uint32_t b = 0; b < X::kGroups; b++) s[b] = next[b];
                 t++, buffer ^= X::kBytes, present_next = present_after;
             }
@@ -703,24 +704,24 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
         char* values = keys + X::kBytes;
         if (t < tile_end) {
             Raw k, v;
-            fetch(t, k_at, k_scale, k_from8, k);
-            fetch(t, v_at, v_scale, v_from8, v);
+            fetch(t, k_at, k_scale, a.k_token, k);
+            fetch(t, v_at, v_scale, a.v_token, v);
             for (; t < tile_end; t += step) {
                 const uint64_t present = keys_there(t);
                 const bool more = t + step < tile_end;
                 typename X::Scores s;
                 typename X::Weights p;
-                put(k, k_to8, keys, kAllKeys);
+                put(k, true, wave * 2 * X::kBytes, kAllKeys);
                 if (more) {
                     if (first_lane(t + step) >= kWave) find_pages(t + step);
-                    fetch(t + step, k_at, k_scale, k_from8, k);
+                    fetch(t + step, k_at, k_scale, a.k_token, k);
                 }
                 wait_lds();
                 x.score(keys, s);
                 scores_masked(t, present, s);
                 x.weights(s, p, a.scale, x.rebase(X::largest(s), a.scale));
-                put(v, v_to8, values, present);
-                if (more) fetch(t + step, v_at, v_scale, v_from8, v);
+                put(v, false, wave * 2 * X::kBytes + X::kBytes, present);
+                if (more) fetch(t + step, v_at, v_scale, a.v_token, v);
                 wait_lds();
                 keep_not_finite(t, values);
                 x.template weigh<false>(values, p, s);
