@@ -699,7 +699,8 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
             }
         }
     } else if constexpr (A::kIn8) {
-        // One buffer: this tile's keys go there from registers, and the next ones are asked for; likewise the values.
+        // One buffer: this tile's keys go there from registers, and the next ones are asked for; likewise the values.  (Two tiles ahead, in as many registers as
+        // there are, 96 decodes of up to 8,000 take 112 us for 110.)
         char* keys = buffers;
         char* values = keys + X::kBytes;
         if (t < tile_end) {
@@ -1050,7 +1051,14 @@ static inline void plan_attention(const lsm_attention_t* a, AttentionArgs& p, ui
             // a short pass is over before its parts could be joined (4 decodes behind 512: 9.6 us in one range, 11.4 in five)
             if (keys <= 1024) splits = 1;
             // many ragged requests: ranges of about 1,024 keys each, so that the longest does not run on alone (96 of up to 8,000: 169 us, 204 uncut)
-            else if (items * splits >= 300 && keys > 2048) p.least[s] = 1024 / kSplitKeys, splits = keys / 1024;
+            else if (page_bytes == 2 && most_seen == ~0ull && items * splits >= 300 && keys > 2048) p.least[s] = 1024 / kSplitKeys, splits = keys / 1024;
+            else if ((page_bytes != 2 || most_seen != ~0ull) && keys > 2048) {
+                // Of 8 bits, or with a window: ranges of such a length that there are up to 768 where all requests are as long as the tables are wide, of 256 to
+                // 1,024 keys (2,048 of 8 bits: as many bytes), whole tiles for all waves.  Requests of up to 8,000 tokens in 8 bits, by this rule / by the one above:
+                // 1 of 2 KV heads 16 / 35 us, 16 of 2 heads 20 / 36, 16 of 8 heads 41 / 51, 48 of 2 heads 40 / 45, 96 of 4 heads 105 / 110.
+                const uint64_t range = (items * keys / 768 + 255) / 256 * 256, longest = 2048 / page_bytes;
+                p.least[s] = (uint32_t)((range < 256 ? 256 : range > longest ? longest : range) / kSplitKeys), splits = keys / (p.least[s] * kSplitKeys);
+            }
         }
         const uint64_t most = keys / (p.least[s] * kSplitKeys);
         // A first stage with long ranges: 256 workgroups or a few more leave some compute units with two and the others with one, so more of them, and the
