@@ -56,7 +56,8 @@ typedef struct {
  *   if the block's first row is not new, the request goes on in it: e = max(e, the block's e so far), and where that is more
  *     than it was, the codes of the rows before the first new one become those of their values divided by 2^e
  *   new codes = values / 2^e, rounded once, to nearest, ties to even; infinities and NaN become NaN
- * Magnitudes that would round beyond the largest number of 4 significant bits that dtype holds (61440 in LSM_FP16) become that.
+ * Magnitudes beyond the largest number of 4 significant bits that dtype holds (61440 in LSM_FP16) become that (so that no finite value is infinite when it is read).
+ * Keys are computed as if in 64 bits, so that each code is the nearest one to the formula's value.
  * Rows behind the new ones keep their bytes.  Tokens that no request has, or whose place is below 0, beyond the table or in a page outside
  * [0, n_pages), are not written.  A block belongs to one request: two that write the same one leave bytes and scale of either.
  * The queries of all n_tokens tokens are normed and rotated in the same launch if q is given.
@@ -73,9 +74,11 @@ int lsm_kv_append8(const lsm_rotation_t* how, const lsm_heads_t* k, const void* 
  *   window > 0: the token at place p of its request's sequence (the group's prefix, then the request's own tokens, holes and all) sees
  *     of what it would see otherwise the tokens at places i < sinks and i > p - window.  window = 0: all of it; sinks has to be 0 then.
  *   scales given (both sides): the pages hold 8 bits, their strides count bytes, and all rows are 16-byte aligned (data 16-byte
- *     aligned, strides multiples of 16).  A value is rounded to base.dtype where that does not hold it (LSM_FP16: below 2^-14 and beyond 65504).
+ *     aligned, strides multiples of 16).  A value is rounded to base.dtype where that does not hold it (LSM_FP16: below 2^-14, and beyond 65504, which
+ *     becomes infinite; LSM_BF16: below 2^-126, which becomes 0, and from 2^128 on).
  * With a window every request is worked on by itself: a prefix is read again for each request whose window reaches it.
- * workspace: as for lsm_prefix_attention, of lsm_window_attention_workspace_bytes(a) bytes.  window, sinks: below 2^30.
+ * workspace: as for lsm_prefix_attention, of lsm_window_attention_workspace_bytes(a) bytes.  window, sinks and, with a window,
+ * (prefix_width + own_width) * page_tokens are below 2^30.
  * Errors: LSM_ERR_NULL, LSM_ERR_BAD_ARG, LSM_ERR_WORKSPACE, LSM_ERR_HIP.
  */
 typedef struct {

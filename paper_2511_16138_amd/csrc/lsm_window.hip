@@ -33,7 +33,10 @@ static int check_window(const lsm_window_attention_t* w) {
     if (w == nullptr) return LSM_ERR_NULL;
     if ((w->k_scales.data == nullptr) != (w->v_scales.data == nullptr)) return LSM_ERR_NULL;
     if (w->window >= 1u << 30 || w->sinks >= 1u << 30 || (w->window == 0 && w->sinks != 0)) return LSM_ERR_BAD_ARG;
-    return check_attention(&w->base, (int64_t)element_bytes(w));
+    const int rc = check_attention(&w->base, (int64_t)element_bytes(w));
+    // with a window the kernels have places, and places less windows, in 32 bits
+    if (rc == LSM_OK && w->window != 0 && (w->base.prefix_width + w->base.own_width) * w->base.page_tokens >= 1ull << 30) return LSM_ERR_BAD_ARG;
+    return rc;
 }
 
 template <typename A>

@@ -99,7 +99,7 @@ NO_SCALES = Scales(None, 0, 0, 0)
 
 
 @pytest.mark.parametrize("change, rc", [
-    (dict(k_scales=NO_SCALES), NULL), (dict(v_scales=NO_SCALES), NULL), (dict(sinks=4), BAD), (dict(w=1 << 30), BAD), (dict(w=5, sinks=1 << 30), BAD), (dict(w=1 << 63), BAD),
+    (dict(k_scales=NO_SCALES), NULL), (dict(v_scales=NO_SCALES), NULL), (dict(sinks=4), BAD), (dict(w=1 << 30), BAD), (dict(w=5, sinks=1 << 30), BAD), (dict(w=1 << 63), BAD), (dict(w=9, own_width=1 << 25, prefix_width=1 << 25), BAD),
     (dict(dtype=2), BAD), (dict(head_dim=96), BAD), (dict(page_tokens=8), BAD), (dict(scale=0.0), BAD), (dict(w=7, scale=math.nan), BAD), (dict(q_offsets=None), NULL),
     (dict(own_lens=None), NULL), (dict(k_pages=Pages(None, 1 << 15, 1024, 128)), NULL),
     (dict(k_pages=Pages(AT, 1 << 15, 1024 + 8, 128)), BAD), (dict(v_pages=Pages(AT + 8, 1 << 15, 1024, 128)), BAD),      # 8 bytes are no row's alignment in 8 bits
