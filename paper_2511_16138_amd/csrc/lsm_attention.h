@@ -528,8 +528,9 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
     // of either type, but for what exceeds its range.
     constexpr uint32_t kRows8 = 2 * X::kRowsPerLoad, kWords8 = X::kWords / 2, kLoads8 = 16 / kRows8;
     static_assert(!A::kIn8 || (kSharers == 1 && kLoads8 >= 1), "");
+    typedef uint32_t Word __attribute__((ext_vector_type(4)));
     struct Raw {
-        uint4 word[kMyBlocks][kLoads8 ? kLoads8 : 1];
+        Word word[kMyBlocks][kLoads8 ? kLoads8 : 1];
         uint32_t scale[kMyBlocks];
     };
     // What a lane's loads and stores go by is computed each time: kept in registers it would be spilled.
@@ -545,9 +546,10 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
             const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)addresses, (int)(first + i));
             const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(addresses >> 32), (int)(first + i));
             raw.scale[i] = (uint32_t)__builtin_amdgcn_readlane((int)scales, (int)(first + i));
-            const char* from = reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
+            // In global memory: an address that was a number may be any, and loads from any count as LDS operations too, which the waits below are for.
+            const auto from = reinterpret_cast<const __attribute__((address_space(1))) char*>((uint64_t)hi << 32 | lo);
 #pragma unroll
-            for (uint32_t j = 0; j < kLoads8; j++) raw.word[i][j] = *reinterpret_cast<const uint4*>(from + j * kRows8 * token_stride + offset);
+            for (uint32_t j = 0; j < kLoads8; j++) raw.word[i][j] = *reinterpret_cast<const __attribute__((address_space(1))) Word*>(from + j * kRows8 * token_stride + offset);
         }
     };
     // present: which of the tile's rows there are; zeros in place of the others
@@ -559,7 +561,7 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
             const float scale = __uint_as_float(raw.scale[i]);
 #pragma unroll
             for (uint32_t j = 0; j < kLoads8; j++) {
-                const uint4 v = raw.word[i][j];
+                const Word v = raw.word[i][j];
                 const uint32_t r = j * kRows8 + l / kWords8;  // of the block; tiles begin with whole blocks, so LDS words are permuted by this number
                 x8 lo = Half<kType>::decode8(v.x, v.y, scale), hi = Half<kType>::decode8(v.z, v.w, scale);
                 if (present != kAllKeys && !((present >> ((kWide ? wave : i) * 16 + r)) & 1)) lo = x8{}, hi = x8{};  // the scale may be NaN, too
@@ -700,7 +702,7 @@ __device__ __forceinline__ void attend(const A& a, const Item& w, uint32_t kv_he
         }
     } else if constexpr (A::kIn8) {
         // One buffer: this tile's keys go there from registers, and the next ones are asked for; likewise the values.  (Two tiles ahead, in as many registers as
-        // there are, 96 decodes of up to 8,000 take 112 us for 110.)
+        // there are, 96 decodes of up to 8,000 take 107 us for 105.)
         char* keys = buffers;
         char* values = keys + X::kBytes;
         if (t < tile_end) {

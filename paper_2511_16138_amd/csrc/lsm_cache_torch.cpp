@@ -403,12 +403,11 @@ PyObject* copy_pages(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return call(n, 3, [&]() -> PyObject* {
         check_constants(o + 1, kCopyPages, 2);
         const std::vector<PyObject*> list = items(o[0], "pages");
-        const at::Tensor &sources = tensor(o[1], "sources"), &targets = tensor(o[2], "targets");
+        const at::Tensor& sources = tensor(o[1], "sources");
         const c10::DeviceIndex device = device_for(sources, "sources");
         check_device(sources, "sources", device);
         if (sources.dim() != 1) throw BadArgument("sources must be int32 [n], is " + shape_text(sources));
         const int32_t *from = ints<int32_t>(o[1], "sources", device, {sources.size(0)}), *to = ints<int32_t>(o[2], "targets", device, {sources.size(0)});
-        (void)targets;
         if (list.empty()) return none();
         const at::Tensor& first = tensor(list[0], "pages");
         if (first.dim() < 1) throw BadArgument("pages must be [n_pages, ...]");

@@ -38,7 +38,7 @@ def values(codes, scales, dtype):
     return out
 
 
-def compare(lsm, q, held, parts, *, scales=None, window=0, sinks=0, scale=None, blocks=None, way=None, joined=None, finite_lse=True):
+def compare(lsm, q, held, parts, *, scales=None, window=0, sinks=0, scale=None, blocks=None, way=None, joined=None):
     """held: pages as they lie on the GPU, blocks: what they hold."""
     blocks = held if blocks is None else blocks
     reference = pages.attention if window else ref.attention
