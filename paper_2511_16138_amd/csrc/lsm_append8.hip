@@ -57,11 +57,12 @@ __device__ __forceinline__ double inverse_root(double x) {
 // two codes (one in 10^5 of them).  That is about 20 instructions an element, and waves of 90 registers, 20 of them on a compute unit, keep enough loads
 // under way beside them: 16,384 tokens of 32 + 2 * 8 heads take 91 us (78 at a copy's rate, 83 in 32 bits).  With the rows in registers a wave has 140 and more of
 // these, and the same takes 105 to 136 us.
-// kMode: 0 = pairs half the rotated part apart, a whole number of lanes; 1 = pairs of neighbours; both with aligned rows and weights of the elements' type; 2 = anything else.
+// kMode: 0 = pairs half the rotated part apart, a whole number of lanes; 1 = pairs of neighbours; both with aligned rows and weights of the elements' type; 2 = anything
+// else; 3, 4 = as 0 and 1, with weights of 32 bits for elements of 16 (16,384 tokens: 107 us for 97 with 16 bits, in the same run; by the way for anything 388).
 template <int kType, int kLanes, int kMode>
 __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave, float* staged) {
     typedef typename Element<kType>::type T;
-    constexpr int E = kEach<T>;
+    constexpr int E = kEach<T>, kPairs = kMode >= 3 ? kMode - 3 : kMode;
     constexpr uint32_t kRows = kWave / kLanes, kSteps = LSM_SCALE_TOKENS / kRows;  // rows at a time
     static_assert(kRows * kSteps == LSM_SCALE_TOKENS, "");
     const uint32_t lane = threadIdx.x & (kWave - 1), sub = lane / kLanes, e0 = (lane & (kLanes - 1)) * E;
@@ -105,7 +106,7 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
         const uint32_t row = step * kRows + sub;
         Lane<T> x;
         if (is_new(row) && inside) {
-            x = load_lane<T>(in + (int64_t)row * s.in_token, kMode != 2 || (a.wide & 1));
+            x = load_lane<T>(in + (int64_t)row * s.in_token, kPairs != 2 || (a.wide & 1));
         } else {
 #pragma unroll
             for (int j = 0; j < E; j++) x.v[j] = (T)0.f;
@@ -134,15 +135,15 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
     if (normed || (keys && r.table != nullptr)) {
         const bool turns = r.table != nullptr && e0 < r.rot_dim;
         const uint32_t half = r.rot_dim >> 1;
-        const bool by_lane = kMode == 0 || (kMode == 2 && !r.interleaved && half % E == 0), neighbours = kMode == 1 || (kMode == 2 && r.interleaved);
+        const bool by_lane = kPairs == 0 || (kPairs == 2 && !r.interleaved && half % E == 0), neighbours = kPairs == 1 || (kPairs == 2 && r.interleaved);
         const int other = turns && by_lane ? (int)(e0 < half ? lane + half / E : lane - half / E) : (int)lane;
         const double mean_by = 1.0 / (double)r.head_dim;
-        constexpr bool kWhole = kType != LSM_FP32 && kMode != 2;  // weights of 16 bits, as the elements: 32 bits hold their products whole
+        constexpr bool kWhole = kType != LSM_FP32 && kMode < 2;  // weights of 16 bits, as the elements: 32 bits hold their products whole
         float weight[E], weight_z[E];  // of this lane's elements, and of the others of their pairs
 #pragma unroll
         for (int j = 0; j < E; j++) weight[j] = 1.f;
         if (normed && inside) {
-            if (sizeof(T) == 4 || (kMode == 2 && r.weight_fp32)) {
+            if (sizeof(T) == 4 || (kMode >= 2 && r.weight_fp32)) {
 #pragma unroll
                 for (int j = 0; j < E; j++) weight[j] = static_cast<const float*>(a.weight)[e0 + j];
             } else {
@@ -164,12 +165,12 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
 #pragma unroll
             for (int j = 0; j < E; j++) cosine[j] = 1.f, sine[j] = 0.f;
             if (turn) {
-                if (kMode == 1) {
+                if (kPairs == 1) {
                     typedef float few __attribute__((ext_vector_type(E / 2)));
                     const few c = *reinterpret_cast<const few*>(angles + e0 / 2), n = *reinterpret_cast<const few*>(angles + half + e0 / 2);
 #pragma unroll
                     for (int j = 0; j < E; j++) cosine[j] = c[j / 2], sine[j] = j & 1 ? n[j / 2] : -n[j / 2];
-                } else if (kMode == 0) {
+                } else if (kPairs == 0) {
                     const uint32_t at = e0 < half ? e0 : e0 - half;
 #pragma unroll
                     for (int j = 0; j < E; j += 4) {
@@ -206,7 +207,7 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
             for (int j = 0; j < E; j++) weighed[j] = kWhole ? y[j] * weight[j] : y[j];
 #pragma unroll
             for (int j = 0; j < E; j++) z[j] = neighbours ? weighed[j ^ 1] : by_lane ? __shfl(weighed[j], other, kWave) : 0.f;
-            if (kMode == 2 && turn && !neighbours && !by_lane) {  // the other element of the pair is in no whole lane: read again
+            if (kPairs == 2 && turn && !neighbours && !by_lane) {  // the other element of the pair is in no whole lane: read again
                 const T* row = in - e0 + (int64_t)(step * kRows + sub) * s.in_token;
 #pragma unroll
                 for (int j = 0; j < E; j++) {
@@ -250,12 +251,12 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
 #pragma unroll 1
         for (uint32_t row = sub; row < row0; row += kRows) {
             uint8_t* at = rows + (int64_t)row * s.token;
-            Codes<E> c = load_codes<E>(at, kMode != 2 || (a.wide & 2));
+            Codes<E> c = load_codes<E>(at, kPairs != 2 || (a.wide & 2));
             float x[E];
             decode(c, x);
 #pragma unroll
             for (int j = 0; j < E; j++) x[j] *= by;
-            store_codes<E>(at, encode<E>(x), kMode != 2 || (a.wide & 2));
+            store_codes<E>(at, encode<E>(x), kPairs != 2 || (a.wide & 2));
         }
     }
     const float by = power_of_two(127 - (int)scale);
@@ -268,7 +269,7 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
             const float4 v = *reinterpret_cast<const float4*>(mine + step * kRows * kLanes * E + j);  // as this lane left it
             y[j] = v.x * by, y[j + 1] = v.y * by, y[j + 2] = v.z * by, y[j + 3] = v.w * by;
         }
-        if (is_new(row) && inside) store_codes<E>(rows + (int64_t)row * s.token, encode<E>(y), kMode != 2 || (a.wide & 2));
+        if (is_new(row) && inside) store_codes<E>(rows + (int64_t)row * s.token, encode<E>(y), kPairs != 2 || (a.wide & 2));
     }
     if (lane == 0) *scale_at = (uint8_t)scale;
 }
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(256) append8_kernel(const Append8Args a) {
     } else {
         const uint32_t wave = (blockIdx.x - before) * 4 + in_group;
         if constexpr (kMode == 2) rotate_any<kType, kLanes>(a.rotate, wave);
-        else rotate_aligned<kType, kLanes, kMode == 1>(a.rotate, wave);
+        else rotate_aligned<kType, kLanes, kMode == 1 || kMode == 4>(a.rotate, wave);
     }
 }
 
@@ -303,6 +304,11 @@ static int set_side(Side& s, const lsm_rotation_t* how, const lsm_heads_t* in, c
 
 template <int kType, int kLanes>
 static void launch_lanes(const Append8Args& a, int mode, uint32_t blocks, hipStream_t stream) {
+    if constexpr (kType != LSM_FP32) {
+        if (mode == 3) hipLaunchKernelGGL((append8_kernel<kType, kLanes, 3>), dim3(blocks), dim3(256), 0, stream, a);
+        if (mode == 4) hipLaunchKernelGGL((append8_kernel<kType, kLanes, 4>), dim3(blocks), dim3(256), 0, stream, a);
+        if (mode >= 3) return;
+    }
     if (mode == 0) hipLaunchKernelGGL((append8_kernel<kType, kLanes, 0>), dim3(blocks), dim3(256), 0, stream, a);
     else if (mode == 1) hipLaunchKernelGGL((append8_kernel<kType, kLanes, 1>), dim3(blocks), dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((append8_kernel<kType, kLanes, 2>), dim3(blocks), dim3(256), 0, stream, a);
@@ -352,8 +358,9 @@ extern "C" int lsm_kv_append8(const lsm_rotation_t* how, const lsm_heads_t* k, c
         if (!rows_aligned(s.in, si, 2, how->dtype)) a.wide &= ~1u;
         if ((reinterpret_cast<uint64_t>(s.pages) | (uint64_t)s.page | (uint64_t)s.token | (uint64_t)s.head) % each != 0) a.wide &= ~2u;
     }
-    const bool aligned = (how->dtype == LSM_FP32 || how->weight_dtype == how->dtype) && a.wide == 3 && (reinterpret_cast<uint64_t>(r.table) & 15) == 0 && (r.part[0].heads == 0 || r.part[0].wide == 3);
-    const int mode = aligned && !r.interleaved && r.rot_dim % (2 * each) == 0 ? 0 : aligned && r.interleaved && r.rot_dim % each == 0 ? 1 : 2;
+    const bool aligned = a.wide == 3 && (reinterpret_cast<uint64_t>(r.table) & 15) == 0 && (r.part[0].heads == 0 || r.part[0].wide == 3);
+    const int more = how->weight_dtype != how->dtype && k_weight != nullptr ? 3 : 0;
+    const int mode = aligned && !r.interleaved && r.rot_dim % (2 * each) == 0 ? more : aligned && r.interleaved && r.rot_dim % each == 0 ? more + 1 : 2;
     // A launch has fewer than 2^32 threads (one of more is cut without an error): more tiles than that take several, the queries go with the first.
     const uint64_t tiles = any ? how->n_tokens / LSM_SCALE_TOKENS + 2 * to->n_requests : 0;
     const uint64_t query_groups = r.part[0].heads != 0 ? (how->n_tokens * r.slices + 3) / 4 : 0;

@@ -111,6 +111,18 @@ def test_append8(lsm, case):
     run(lsm, gen, fused, hq, hkv, d, q_lens, own_lens, page, table=table, positions=positions, weights=weights, interleaved=interleaved, eps=1e-5)
 
 
+@pytest.mark.parametrize("d, rot, dtype, interleaved", [(128, 128, BF16, False), (64, 32, FP16, True), (256, 64, FP16, False), (128, 64, BF16, True), (64, 64, BF16, False)])
+def test_weights_of_32_bits(lsm, d, rot, dtype, interleaved):
+    """Elements of 16 bits with weights of 32, rows aligned: kernels of their own, on every kind of pair."""
+    gen = torch.Generator().manual_seed(d + rot)
+    q_lens, own_lens, hq, hkv = [40, 1, 33, 0, 5], [47, 16, 33, 4, 70], 4, 2
+    n = sum(q_lens)
+    fused = normal(gen, (n, hq + 2 * hkv, d), dtype)
+    table = lsm.lsm_rope_table(300, rot).cpu()
+    positions = torch.randint(0, 300, (n,), generator=gen, dtype=torch.int32)
+    run(lsm, gen, fused, hq, hkv, d, q_lens, own_lens, 16, table=table, positions=positions, weights=[normal(gen, (d,), FP32) for _ in range(2)], interleaved=interleaved)
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
 def test_values_as_they_are_are_rounded_exactly(lsm, dtype):
     """No norm, no rotation: codes are the nearest ones, ties to even; magnitudes of every size, ties, subnormals, zeros."""
