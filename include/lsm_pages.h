@@ -76,8 +76,9 @@ int lsm_kv_append8(const lsm_rotation_t* how, const lsm_heads_t* k, const void* 
  *   scales given (both sides): the pages hold 8 bits, their strides count bytes, and all rows are 16-byte aligned (data 16-byte
  *     aligned, strides multiples of 16).  A value is rounded to base.dtype where that does not hold it (LSM_FP16: below 2^-14, and beyond 65504, which
  *     becomes infinite; LSM_BF16: below 2^-126, which becomes 0, and from 2^128 on).
- * With a window every request is worked on by itself: a prefix is read again for each request whose window reaches it.
- * workspace: as for lsm_prefix_attention, of lsm_window_attention_workspace_bytes(a) bytes.  window, sinks and, with a window,
+ * With a window that is shorter than the tables ((prefix_width + own_width) * page_tokens) every request is worked on by itself: a prefix is read again
+ * for each request whose window reaches it.
+ * workspace: as for lsm_prefix_attention, of lsm_window_attention_workspace_bytes(a) bytes.  window, sinks and, with such a window,
  * (prefix_width + own_width) * page_tokens are below 2^30.
  * Errors: LSM_ERR_NULL, LSM_ERR_BAD_ARG, LSM_ERR_WORKSPACE, LSM_ERR_HIP.
  */

@@ -199,7 +199,8 @@ def test_a_window_dealt_to_several_workgroups(lsm, hkv, q_lens, own, way, in_8_b
         held, scales = to_8_bits(gen, blocks)
         blocks, more = values(held, scales, BF16), dict(scales=scales)
     for window, sinks, joined in ((3000, 500, True), (2100, 1, True), (1 << 20, 3, True), (150, 4, way == 2 and None)):
-        compare(lsm, q, held, parts, blocks=blocks, window=window, sinks=sinks, way=way, joined=joined, **more)
+        # a window as long as the tables hides nothing: the kernels without one
+        compare(lsm, q, held, parts, blocks=blocks, window=window, sinks=sinks, way=way if window < 1 << 20 else None, joined=joined, **more)
 
 
 @pytest.mark.parametrize("in_8_bits", [False, True])
