@@ -54,8 +54,8 @@ __device__ __forceinline__ double inverse_root(double x) {
 // One wave has a block of 16 tokens of one head, keys or values: kLanes lanes of 16 bytes hold a row, and the rows wait in LDS until the largest magnitude is known, so
 // every byte is read once and written once.  No other wave writes any of the block, nor its scale.
 // Keys are normed and rotated in 64 bits: a code is the nearest one to the formula's value then, and not to one that 32 bits have moved across the border between
-// two codes (one in 10^5 of them).  That is about 20 instructions an element, and waves of 90 registers, 20 of them on a compute unit, keep enough loads
-// under way beside them: 16,384 tokens of 32 + 2 * 8 heads take 91 us (78 at a copy's rate, 83 in 32 bits).  With the rows in registers a wave has 140 and more of
+// two codes (one in 10^5 of them).  That is about 20 instructions an element, and waves of 90 registers (fp16; 121 to 127 in bf16), 20 of them (16) on a compute unit, keep enough
+// loads under way beside them: 16,384 tokens of 32 + 2 * 8 heads take 92.6 us in bf16 (78 at a copy's rate, 83 in 32 bits).  With the rows in registers a wave has 140 and more of
 // these, and the same takes 105 to 136 us.
 // kMode: 0 = pairs half the rotated part apart, a whole number of lanes; 1 = pairs of neighbours; both with aligned rows and weights of the elements' type; 2 = anything
 // else; 3, 4 = as 0 and 1, with weights of 32 bits for elements of 16 (16,384 tokens: 107 us for 97 with 16 bits, in the same run; by the way for anything 388).
@@ -138,7 +138,7 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
         const bool by_lane = kPairs == 0 || (kPairs == 2 && !r.interleaved && half % E == 0), neighbours = kPairs == 1 || (kPairs == 2 && r.interleaved);
         const int other = turns && by_lane ? (int)(e0 < half ? lane + half / E : lane - half / E) : (int)lane;
         const double mean_by = 1.0 / (double)r.head_dim;
-        constexpr bool kWhole = kType != LSM_FP32 && kMode < 2;  // weights of 16 bits, as the elements: 32 bits hold their products whole
+        constexpr bool kWhole = kType != LSM_FP32 && kMode < 2;  // weights of 16 bits, as the elements: 32 bits hold the bits of their products, and fp16's exponents
         float weight[E], weight_z[E];  // of this lane's elements, and of the others of their pairs
 #pragma unroll
         for (int j = 0; j < E; j++) weight[j] = 1.f;
@@ -205,6 +205,28 @@ __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave
             }
 #pragma unroll
             for (int j = 0; j < E; j++) weighed[j] = kWhole ? y[j] * weight[j] : y[j];
+            if constexpr (kWhole && kType == LSM_BF16) {
+                // The product of two bfloat16 has 16 bits, but its exponent may leave the range of 32 bits, however ordinary it is once divided by the root: rows with
+                // such products have them in 64 bits, and so have rows with zeros, which are not told apart.  (64 bits for all rows: 16,384 tokens 109 us for 92.6; without
+                // the look 91.3.)
+                float least = 1.f, largest = 0.f;
+#pragma unroll
+                for (int j = 0; j < E; j++) least = fminf(least, __builtin_fabsf(weighed[j])), largest = fmaxf(largest, __builtin_fabsf(weighed[j]));
+                if (normed && __any(is_new(step * kRows + sub) && inside && !(least >= 0x1p-126f && largest < __builtin_inff()))) {
+#pragma unroll
+                    for (int j = 0; j < E; j++) {
+                        double x = (double)y[j] * (double)weight[j];
+                        const double pair = neighbours ? (double)y[j ^ 1] * (double)weight[j ^ 1] : by_lane ? __shfl(x, other, kWave) : 0.0;
+                        if (turn && e0 + j < r.rot_dim) {
+                            x = x * (double)cosine[j] + pair * (double)sine[j];
+                            if (!known) x = __builtin_nan("");
+                        }
+                        z[j] = to_odd(x * by);
+                    }
+                    keep(step, z);
+                    continue;
+                }
+            }
 #pragma unroll
             for (int j = 0; j < E; j++) z[j] = neighbours ? weighed[j ^ 1] : by_lane ? __shfl(weighed[j], other, kWave) : 0.f;
             if (kPairs == 2 && turn && !neighbours && !by_lane) {  // the other element of the pair is in no whole lane: read again
