@@ -1,5 +1,5 @@
-"""Codes of normed and rotated keys are the nearest ones to the formula's values (tests/nearest_codes.py): a million of each way through the kernels, of which
-computation in 32 bits gets about ten wrong (tests/test_nearest_codes.py), and values next to a border."""
+"""Codes of normed and rotated keys are the nearest ones to the formula's values (tests/nearest_codes.py): four million of each way through the kernels, of
+which computation in 32 bits gets several wrong (tests/test_nearest_codes.py), and values next to a border."""
 import pytest
 import torch
 
@@ -60,7 +60,7 @@ def test_codes_are_the_nearest(lsm, way):
     dtype, weight_dtype, d, rot, interleaved, aligned = way
     gen = torch.Generator().manual_seed(d * 1000 + rot + interleaved)
     heads = 4
-    n = (1 << 20) // (heads * d) // 16 * 16
+    n = (1 << 22) // (heads * d) // 16 * 16
     x = torch.randn((n, heads, d), generator=gen).to(dtype)
     weight = None if weight_dtype is None else (1 + 0.2 * torch.randn(d, generator=gen)).to(weight_dtype)
     table, positions = lsm.lsm_rope_table(4096, rot).cpu(), torch.randint(0, 4096, (n,), generator=gen, dtype=torch.int32)
