@@ -55,11 +55,11 @@ __device__ __forceinline__ double inverse_root(double x) {
 // One wave has a block of 16 tokens of one head, keys or values: kLanes lanes of 16 bytes hold a row, and the rows wait in LDS until the largest magnitude is known, so
 // every byte is read once and written once.  No other wave writes any of the block, nor its scale.
 // Keys are normed and rotated in 64 bits: a code is the nearest one to the formula's value then, and not to one that 32 bits have moved across the border between
-// two codes (one in 10^5 of them).  That is about 20 instructions an element, and waves of 90 registers (fp16; 121 to 127 in bf16), 20 of them (16) on a compute unit, keep enough
+// two codes (one to three in a million).  That is about 20 instructions an element, and waves of 90 registers (fp16; 121 to 127 in bf16), 20 of them (16) on a compute unit, keep enough
 // loads under way beside them: 16,384 tokens of 32 + 2 * 8 heads take 92.6 us in bf16 (78 at a copy's rate, 83 in 32 bits).  With the rows in registers a wave has 140 and more of
 // these, and the same takes 105 to 136 us.
 // kMode: 0 = pairs half the rotated part apart, a whole number of lanes; 1 = pairs of neighbours; both with aligned rows and weights of the elements' type; 2 = anything
-// else; 3, 4 = as 0 and 1, with weights of 32 bits for elements of 16 (16,384 tokens: 107 us for 97 with 16 bits, in the same run; by the way for anything 388).
+// else; 3, 4 = as 0 and 1, with weights of 32 bits for elements of 16 (16,384 tokens: 107 us for 93 with 16 bits; by the way for anything 388).
 template <int kType, int kLanes, int kMode>
 __device__ __forceinline__ void append_block(const Append8Args& a, uint32_t wave, float* staged) {
     typedef typename Element<kType>::type T;

@@ -1074,7 +1074,8 @@ static inline void plan_attention(const lsm_attention_t* a, AttentionArgs& p, ui
         // A first stage with long ranges: 256 workgroups or a few more leave some compute units with two and the others with one, so more of them, and the
         // fewer the longer the second stage is (at 5 TB/s beside 1 PFLOP/s), which shares the compute units with them.  256 decodes behind 8,192 and
         // 16,384, 2 KV heads: 15 own tokens each 119 -> 90 us, 1,024 each 117 -> 93 with 410 of them; 2,047 each 127 with 256 or 410, 120 with 340.
-        // Behind 4,096 and 8,192 with 2,047 each: 93 with 256, 101 with 340.
+        // Behind 4,096 and 8,192 with 2,047 each: 93 with 256, 101 with 340.  Own keys count as 16 bits in 8 too: by their bytes the first batch with 2,047 each would
+        // have 410, 116 us for 113.
         if (s == 0 && p.wide[0]) {
             const bool alone = a->n_requests * own_keys * 200 < rows * prefix_keys;
             const uint64_t more = (alone ? 410 : 340) / (p.tiles[0] * a->kv_heads);

@@ -3,10 +3,10 @@
 // The kernels are those of lsm_attention.h.  Of 8 bits, rows are converted to dtype on their way into LDS, once for all waves that use them; with a window, tiles between the first tokens
 // and the window are left out.  Measured, with the floor of bytes at a copy's 4.94 TB/s or of operations at a library product's 1.38 PFLOP/s:
 //   96 decodes of up to 8,000 keys, 4 KV heads of 128, 8 bits    104 us, 4.2 TB/s      (88: memory, and the starts and ends of ranges)
-//   256 decodes behind 8,192 and 16,384, 2 heads, 8 bits         112 us, 0.53 PFLOP/s  (43: matrix cores and vector units on the prefixes)
-//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096, 8 bits      1,100 us, 0.91 PFLOP/s (728: as in 16 bits, and the conversion, a tenth)
+//   256 decodes behind 8,192 and 16,384, 2 heads, 8 bits         113 us, 0.52 PFLOP/s  (43: no unit is busy half of the time)
+//   8 prompts of 1,024 - 2,048 behind 1,536 - 4,096, 8 bits      1,098 - 1,157 us by card, 0.87 - 0.92 PFLOP/s (728: as in 16 bits, and the conversion, a tenth)
 //   64 decodes of up to 16,000 keys, window 1,024, 16 bits       57 us, 4.7 TB/s       (54: memory)
-//   6 prompts of 200 - 3,000, window 512, 8 bits                 205 us, 0.52 PFLOP/s  (78: a tile of rows sees 8.3 of its 11 tiles of keys, and starts and ends)
+//   6 prompts of 200 - 3,000, window 512, 8 bits                 204 - 210 us, 0.52 PFLOP/s  (78: a tile of rows sees 8.3 of its 11 tiles of keys, and starts and ends)
 #include <hip/hip_runtime.h>
 
 #include "lsm_attention.h"
@@ -35,7 +35,7 @@ static void launch_head(const A& p, uint32_t head, uint32_t blocks, hipStream_t 
 static bool in_8_bits(const lsm_window_attention_t* w) { return w->k_scales.data != nullptr; }
 static uint64_t element_bytes(const lsm_window_attention_t* w) { return in_8_bits(w) ? 1 : 2; }
 // Whether the window can hide anything: where the tables hold no more than it, the calls without one are the same, and read a shared prefix once for all requests
-// (256 decodes behind prefixes of 8,192 and 16,384 in 8 bits: 259 us with a window of 2^20 worked on request by request, 112 without one).
+// (256 decodes behind prefixes of 8,192 and 16,384 in 8 bits: 259 us with a window of 2^20 worked on request by request, 113 without one).
 static bool hides(const lsm_window_attention_t* w) { return w->window != 0 && w->window < (w->base.prefix_width + w->base.own_width) * w->base.page_tokens; }
 // The keys that a tile of rows reaches: the windows of up to 128 tokens, the first tokens, and what the ends of either have in a unit.
 static uint64_t most_seen(const lsm_window_attention_t* w) { return hides(w) ? w->window + w->sinks + 128 + 2 * kSplitKeys : ~0ull; }
